@@ -10,6 +10,7 @@
 #ifndef DARE_KERNELS_H
 #define DARE_KERNELS_H
 
+#include <stddef.h>
 #include <stdint.h>
 #include "dare.h"
 
@@ -150,6 +151,95 @@ dare_status dare_k_norm(int dtype, int kind, const void* x, const void* gain,
 /* Residual sum out = x + o over n_elems elements (a multiple of 8) of dtype. */
 dare_status dare_k_residual_add(int dtype, const void* x, const void* o, void* out,
                                 long n_elems, void* hip_stream);
+
+/*
+ * Operators of a decoder layer whose query heads share key heads, with biases, sequences of different lengths and
+ * caches that reach behind the tokens of a call.  Sizes of 0 tokens are fine (nothing is enqueued); every ld is the
+ * distance of two rows in elements, and what is read or written by rows lies on 16-byte boundaries (pointers, and ld times
+ * the size of an element) unless it says otherwise.  dare_last_error(NULL) has the text of a refusal.
+ */
+enum { DARE_ACT_NONE = 0, DARE_ACT_SILU = 1, DARE_ACT_GELU = 2, DARE_ACT_GELU_TANH = 3 };
+
+/*
+ * Projection with its epilogue, one rounding at the end:
+ *     out[t, 0:n] = act(a[t, 0:k] . W + bias) + residual[t, 0:n]        for t in [0, m)
+ * act: none; silu z / (1 + e^-z); gelu z Phi(z); its tanh form z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.
+ *   a [m, lda], residual [m, ldr] (or NULL), out [m, ldo] dtype; wt [n, k] (packed weight), bias [n] (or NULL) dtype
+ * out may be residual (with the same ld); it must not overlap a.  k and n are multiples of 64.
+ * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, unknown act), UNSUPPORTED (k or n not a
+ * multiple of 64).
+ */
+dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, int n, int k, int m, const void* bias,
+                          int act, const void* residual, long ldr, void* out, long ldo, void* hip_stream);
+
+/*
+ * Rotary embedding by positions, with the cache rows it leads to.  Pair i of the first rot_dim channels of every head,
+ * (a, b) = channels (2i, 2i + 1) for DARE_ROPE_PAIRS, (i, i + rot_dim / 2) for DARE_ROPE_HALF, becomes
+ *     magnitude * (a cos - b sin, b cos + a sin),  angle = pos[t] * freqs[i] (formed and reduced in 64 bits);
+ * channels from rot_dim on go through as they are.
+ *   pos    [n_tokens] int32, any value           freqs  [rot_dim / 2] fp64 (dare_k_rope_freqs)
+ *   q      [n_tokens, ldq], n_heads heads, rotated into q_out [n_tokens, ldqo]
+ *   k      [n_tokens, ldk], n_kv_heads heads, rotated into k_out
+ *   v      [n_tokens, ldv], n_kv_heads heads, copied into v_out
+ *   rows   NULL: k_out and v_out have a row per token.  Else [n_tokens] int32: token t goes to row rows[t] of them, nowhere if that is
+ *          outside [0, out_rows); no two tokens to the same row
+ * Each of q, k and v may be NULL (with its output).  q_out may be q, and without rows k_out k and v_out v (with the same
+ * ld); there is no other overlap.  head_dim is a multiple of 8 up to 256, rot_dim even, 2 .. head_dim.  Alignment that is less than 16
+ * bytes, and halves of which no 16 bytes have their partners in 16, are taken element by element.
+ */
+enum { DARE_ROPE_HALF = 0, DARE_ROPE_PAIRS = 1 };
+dare_status dare_k_rope(int dtype, int layout, int n_tokens, int head_dim, int rot_dim, const int32_t* pos,
+                        const double* freqs, float magnitude, const void* q, long ldq, void* q_out, long ldqo, int n_heads,
+                        const void* k, long ldk, void* k_out, long ldko, const void* v, long ldv, void* v_out, long ldvo,
+                        int n_kv_heads, const int32_t* rows, int out_rows, void* hip_stream);
+
+/*
+ * Frequencies for dare_k_rope: f_i = base^(-2i / rot_dim), changed for contexts longer than the trained one by `factor`:
+ *   DARE_ROPE_SCALE_NONE    as they are
+ *   DARE_ROPE_SCALE_LINEAR  f_i / factor (interpolated positions)
+ *   DARE_ROPE_SCALE_BASE    base * factor^(rot_dim / (rot_dim - 2)) instead of base (rot_dim above 2): the slowest pair is interpolated,
+ *                           the fastest left alone
+ *   DARE_ROPE_SCALE_TURNS   f_i (g + (1 - g) / factor), g = clamp((turns_i - low) / (high - low), 0, 1), turns_i = context f_i /
+ *                           (2 pi): pairs that turn `high` times in the trained context stay, those that turn `low` times are interpolated
+ * Computed on the HOST in double precision and copied to the device pointer `freqs` (fp64 [rot_dim / 2]) with a
+ * synchronous copy.
+ */
+enum { DARE_ROPE_SCALE_NONE = 0, DARE_ROPE_SCALE_LINEAR = 1, DARE_ROPE_SCALE_BASE = 2, DARE_ROPE_SCALE_TURNS = 3 };
+dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scaling, double factor, double context,
+                              double low, double high);
+
+/*
+ * Attention over packed sequences with shared key heads.  Sequence b has the query tokens q_off[b] .. q_off[b + 1] - 1 and the
+ * keys k_begin[b] .. k_end[b] - 1; its queries are the last len_q of its len_k positions (len_q may be the larger one).
+ *     out[t, h] = softmax_j(scale q[t, h] . k[j, h / G]) v[j, h / G],   G = n_heads / n_kv_heads,
+ * over the keys that the token sees: all of its sequence with causal_block = 0; else those whose position lies in its own
+ * block of causal_block positions or in one before (1: causal).  A token that sees no key gets zeros.  What lies in
+ * keys that a token does not see does not matter, infinities and NaN included.
+ *   q, out       [total_q, ldq or ldo] dtype, n_heads heads of head_dim
+ *   k, v         [k_rows, ldk or ldv] dtype, n_kv_heads heads: packed like the queries, or a cache
+ *   q_off        [batch + 1] int32, ascending from 0; rows of out from q_off[batch] on are left as they are
+ *   k_begin/end  [batch] int32, 0 <= begin <= end <= k_rows.  (Values outside are taken as the nearest inside, so nothing
+ *                outside of q, k and v is read, and nothing outside of out written.)
+ * max_q and max_k, the largest numbers of query tokens and keys of a sequence, choose how the work is cut: a
+ * captured call may be replayed with other lengths.  Longer sequences than they say are right as well, only slower.
+ * workspace: dare_k_attention_packed_workspace() bytes (for the same config), 16-byte aligned, needed while the call runs, not
+ * initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
+ * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, n_heads not a multiple of n_kv_heads, scale not above 0 or not
+ * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; total_q * n_heads + 128 batch, or the grid, beyond
+ * 2^31).
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(dare_packed_config) */
+  int32_t dtype, batch, total_q, k_rows, max_q, max_k;
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t causal_block;
+  float scale;
+  int64_t ldq, ldk, ldv, ldo;
+} dare_packed_config;
+dare_status dare_k_attention_packed_workspace(const dare_packed_config* cfg, size_t* bytes);
+dare_status dare_k_attention_packed(const dare_packed_config* cfg, const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* q_off, const int32_t* k_begin, const int32_t* k_end, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -29,9 +29,13 @@ EXPORTS = (
     "dare_model_create", "dare_model_set_layer", "dare_model_set_io", "dare_model_set_rule",
     "dare_model_set_prefix", "dare_model_step", "dare_model_logits", "dare_model_layer",
     "dare_model_destroy", "dare_model_last_error",
+    "dare_k_linear", "dare_k_rope", "dare_k_rope_freqs", "dare_k_attention_packed", "dare_k_attention_packed_workspace",
 )
 RULE_SCORE, RULE_QUANTILE = 0, 1
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+ACTIVATIONS = {None: 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "turns": 3}
 NORM_KINDS = {None: NORM_NONE, "layer": NORM_LAYER, "rms": NORM_RMS}
 
 
@@ -71,6 +75,18 @@ class DareModelConfig(ctypes.Structure):
         ("rope_base", ctypes.c_float),
         ("device", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
+    ]
+
+
+class DarePackedConfig(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("total_q", ctypes.c_int32), ("k_rows", ctypes.c_int32),
+        ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
+        ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("causal_block", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64),
     ]
 
 
@@ -170,6 +186,18 @@ def lib():
     L.dare_set_prefix.restype = i32
     L.dare_k_quantile_mask.argtypes = [vp, i32, i32, f32, i32, vp, vp, vp, vp, vp]
     L.dare_k_quantile_mask.restype = i32
+    lng = ctypes.c_long
+    L.dare_k_linear.argtypes = [i32, vp, lng, vp, i32, i32, i32, vp, i32, vp, lng, vp, lng, vp]
+    L.dare_k_linear.restype = i32
+    L.dare_k_rope.argtypes = ([i32] * 5 + [vp, vp, f32] + [vp, lng, vp, lng, i32] + [vp, lng, vp, lng] * 2 + [i32] +
+                              [vp, i32, vp])
+    L.dare_k_rope.restype = i32
+    L.dare_k_rope_freqs.argtypes = [vp, i32, ctypes.c_double, i32] + [ctypes.c_double] * 4
+    L.dare_k_rope_freqs.restype = i32
+    L.dare_k_attention_packed.argtypes = [ctypes.POINTER(DarePackedConfig)] + [vp] * 8 + [ctypes.c_size_t, vp]
+    L.dare_k_attention_packed.restype = i32
+    L.dare_k_attention_packed_workspace.argtypes = [ctypes.POINTER(DarePackedConfig), ctypes.POINTER(ctypes.c_size_t)]
+    L.dare_k_attention_packed_workspace.restype = i32
     _lib = L
     return L
 
@@ -510,6 +538,183 @@ def dare_k_copy_rows(src, dst, idx=None, m_dev=None, stream=None):
     row_bytes = src.shape[-1] * src.element_size()
     _check(lib().dare_k_copy_rows(_ptr(src), _ptr(dst), n_rows, row_bytes, _ptr(idx), _ptr(m_dev),
                                   _stream(stream)))
+
+
+# ---- decoder layers with shared key heads ------------------------------------------------
+
+def _dtype_of(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return DARE_BF16
+    if t.dtype == torch.float32:
+        return DARE_F32
+    raise ValueError("dtype must be bfloat16 or float32, not %s" % t.dtype)
+
+
+def _on_device(like, **tensors):
+    """Every tensor that is given lies on the GPU of `like`."""
+    if not like.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
+
+
+def _heads(name, t, like, n=None, heads=None, head_dim=None):
+    """Pointer and row distance of a [tokens, heads, head_dim] tensor whose heads lie one behind the other."""
+    if t.dim() != 3 or t.dtype != like.dtype:
+        raise ValueError("%s must be [tokens, heads, head_dim] of the queries' dtype" % name)
+    rows, h, d = t.shape
+    if (n is not None and rows != n) or (heads is not None and h != heads) or (head_dim is not None and d != head_dim):
+        raise ValueError("%s has the shape %s" % (name, tuple(t.shape)))
+    if t.numel() and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+        raise ValueError("the heads of a row of %s must lie one behind the other" % name)
+    return t.data_ptr(), t.stride(0) if rows > 1 else h * d
+
+
+def _matrix(name, t, like, rows, cols):
+    """Pointer and row distance of a [rows, cols] tensor with contiguous rows."""
+    if t.shape != (rows, cols) or t.dtype != like.dtype:
+        raise ValueError("%s must be [%d, %d] of dtype %s" % (name, rows, cols, like.dtype))
+    if t.numel() and cols > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _ints(name, t, n):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of %d elements" % (name, n))
+    return t.data_ptr()
+
+
+def _enqueue(like, stream, fn, *args):
+    """fn(*args, stream) with the device of `like` as the current one."""
+    import torch
+    if stream is not None and stream.device != like.device:
+        raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, like.device))
+    if like.device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(like.device):
+            _check(fn(*args, _stream(stream)))
+
+
+def dare_k_linear(a, wt, out, bias=None, act=None, residual=None, stream=None):
+    """out = act(a W + bias) + residual.  a [m, k], out and residual [m, n] with contiguous rows, wt [n, k] packed
+    (dare_k_pack_weight), act None, "silu", "gelu" or "gelu_tanh"; out may be residual."""
+    _on_device(a, wt=wt, out=out, bias=bias, residual=residual)
+    n, k = wt.shape
+    m = a.shape[0]
+    pa, lda = _matrix("a", a, a, m, k)
+    po, ldo = _matrix("out", out, a, m, n)
+    pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, a, m, n)
+    if wt.dtype != a.dtype or not wt.is_contiguous():
+        raise ValueError("wt must be contiguous, of the dtype of a")
+    if bias is not None and (bias.shape != (n,) or bias.dtype != a.dtype or not bias.is_contiguous()):
+        raise ValueError("bias must be [%d] of the dtype of a" % n)
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % list(ACTIVATIONS))
+    _enqueue(a, stream, lib().dare_k_linear, _dtype_of(a), pa, lda, wt.data_ptr(), n, k, m,
+             None if bias is None else bias.data_ptr(), ACTIVATIONS[act], pr, ldr, po, ldo)
+
+
+def dare_k_rope_freqs(rot_dim, base=10000.0, scaling=None, factor=1.0, context=8192, low=1.0, high=4.0, device="cuda"):
+    """Frequencies (float64 [rot_dim / 2] on the device) for dare_k_rope; scaling None, "linear", "base" or "turns"."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s" % list(ROPE_SCALINGS))
+    freqs = torch.empty(max(rot_dim, 2) // 2, dtype=torch.float64, device=device)
+    with torch.cuda.device(freqs.device):
+        _check(lib().dare_k_rope_freqs(_ptr(freqs), rot_dim, float(base), ROPE_SCALINGS[scaling], float(factor),
+                                       float(context), float(low), float(high)))
+    return freqs
+
+
+def dare_k_rope(pos, freqs, layout="half", q=None, q_out=None, k=None, k_out=None, v=None, v_out=None, rows=None,
+                magnitude=1.0, stream=None):
+    """Rotary embedding of q and k [tokens, heads, head_dim] by the positions pos (int32 [tokens]) into q_out and k_out; v is
+    copied into v_out.  rows (int32 [tokens]): the rows of k_out and v_out, for instance of a cache, that the tokens go
+    to.  layout "half" or "pairs"."""
+    import torch
+    first = q if q is not None else k if k is not None else v
+    if first is None:
+        raise ValueError("nothing to rotate")
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError("layout must be one of %s" % list(ROPE_LAYOUTS))
+    _on_device(first, pos=pos, freqs=freqs, q=q, q_out=q_out, k=k, k_out=k_out, v=v, v_out=v_out, rows=rows)
+    n, d = first.shape[0], first.shape[2] if first.dim() == 3 else 0
+    kv = k if k is not None else v
+    args, out_rows = [], 0
+    for name, x, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
+        if (x is None) != (out is None):
+            raise ValueError("%s and %s_out go together" % (name, name))
+        if x is None:
+            args += [None, 0, None, 0]
+            continue
+        heads = None if name == "q" else kv.shape[1] if kv.dim() == 3 else -1
+        args += _heads(name, x, first, n, heads, d)
+        scattered = rows is not None and name != "q"
+        args += _heads(name + "_out", out, first, None if scattered else n, x.shape[1], d)
+        if scattered:
+            if out_rows and out.shape[0] != out_rows:
+                raise ValueError("k_out and v_out must have as many rows as each other")
+            out_rows = out.shape[0]
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous float64 vector")
+    pr = None if rows is None else _ints("rows", rows, n)
+    if rows is not None and (kv is None or out_rows == 0):
+        raise ValueError("rows without k or v, or without rows to write")
+    _enqueue(first, stream, lib().dare_k_rope, _dtype_of(first), ROPE_LAYOUTS[layout], n, d, 2 * freqs.shape[0],
+             _ints("pos", pos, n), freqs.data_ptr(), magnitude, *args[:4], 0 if q is None else q.shape[1], *args[4:],
+             0 if kv is None else kv.shape[1], pr, out_rows)
+
+
+def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, causal_block=0, scale=None,
+                            workspace=None, stream=None):
+    """Attention of packed sequences.  q, out [total_q, n_heads, head_dim], k, v [k_rows, n_kv_heads, head_dim] (parts of one
+    buffer, or a cache); int32 q_off [batch + 1], k_begin and k_end [batch].  causal_block 0: every token sees all keys of its
+    sequence, b: those up to the end of its block of b positions (1: causal).  scale: 1 / sqrt(head_dim).  max_q, max_k: the largest
+    numbers of query tokens and keys of a sequence.  workspace: a uint8 tensor of dare_k_attention_packed_workspace() bytes to
+    use instead of one of the call's own."""
+    _on_device(q, k=k, v=v, out=out, q_off=q_off, k_begin=k_begin, k_end=k_end, workspace=workspace)
+    pq, ldq = _heads("q", q, q)
+    total, h, d = q.shape
+    pk, ldk = _heads("k", k, q, None, None, d)
+    rows, kv, _ = k.shape
+    pv, ldv = _heads("v", v, q, rows, kv, d)
+    po, ldo = _heads("out", out, q, total, h, d)
+    batch = k_begin.shape[0]
+    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), _dtype_of(q), batch, total, rows, max_q, max_k, h, kv, d,
+                           causal_block, d ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
+    ref = ctypes.byref(cfg)
+    offsets = _ints("q_off", q_off, batch + 1), _ints("k_begin", k_begin, batch), _ints("k_end", k_end, batch)
+    need = ctypes.c_size_t()
+    _check(lib().dare_k_attention_packed_workspace(ref, ctypes.byref(need)))
+    if workspace is None and need.value:
+        workspace = _scratch(need.value, q.device, stream)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _enqueue(q, stream, lib().dare_k_attention_packed, ref, pq, pk, pv, po, *offsets, _ptr(workspace), size)
+
+
+def dare_k_attention_packed_workspace(dtype, batch, total_q, max_q, max_k, n_heads, n_kv_heads, head_dim):
+    """Bytes of the workspace of a dare_k_attention_packed call of these sizes (0: none)."""
+    wq, wk = n_heads * head_dim, n_kv_heads * head_dim
+    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), dtype, batch, total_q, 0, max_q, max_k, n_heads, n_kv_heads,
+                           head_dim, 0, 1.0, wq, wk, wk, wq)
+    need = ctypes.c_size_t()
+    _check(lib().dare_k_attention_packed_workspace(ctypes.byref(cfg), ctypes.byref(need)))
+    return need.value
+
+
+def _scratch(n_bytes, device, stream):
+    """Memory for one call, from the pool of the stream that the call runs on: what is freed there is used again behind
+    the call, not beside it."""
+    import torch
+    if stream is None:
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
 
 
 # ---- benchmark aids (libdare_bench.so, include/dare_bench.h) ------------------------------

@@ -1,0 +1,48 @@
+// Which keys a token sees and how attention over packed sequences is cut, as plain arithmetic: no HIP here, so that both
+// can be evaluated over their whole range without a GPU.
+#pragma once
+
+namespace dare {
+
+// Keys that token i of a sequence sees: a prefix of its len_k keys.  shift = len_k - len_q: the queries are the last
+// positions.  block 0: all; else up to the end of the token's block of that many positions.  A token in front of the
+// first key (negative position) sees none.
+constexpr __attribute__((always_inline)) int packed_limit(int i, int shift, int len_k, int block) {
+  if (block == 0) return len_k;
+  const int pos = i + shift;
+  if (pos < 0) return 0;
+  const unsigned end = ((unsigned)pos / (unsigned)block + 1u) * (unsigned)block;  // (at most pos + block < 2^32)
+  return end < (unsigned)len_k ? (int)end : len_k;
+}
+
+// Partial results of a block of `rows` rows: sums [rows][head_dim], references [rows], sums of probabilities [rows]
+constexpr long packed_slot_floats(int head_dim, int rows) { return (long)rows * (head_dim + 2); }
+
+constexpr int kPackedMaxParts = 64;
+
+struct PackedPlan {
+  int rows;       // rows of a block
+  int blocks;     // blocks launched (of every key head)
+  int parts;      // parts of a block's keys, at most
+  int part_keys;  // keys of a part, at least
+};
+
+constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, int group, int n_kv) {
+  PackedPlan plan{};
+  plan.rows = (long)max_q * group <= 16 ? 16 : 32;
+  plan.blocks = (int)((long)total_q * group / plan.rows) + batch;
+  plan.parts = 1;
+  plan.part_keys = 1 << 30;
+  // As many parts as fill the 256 CUs about three times, of 256 keys at least
+  const long pairs = (long)plan.blocks * n_kv;
+  long parts = 768 / (pairs > 0 ? pairs : 1);
+  if (parts > max_k / 256) parts = max_k / 256;
+  if (parts > kPackedMaxParts) parts = kPackedMaxParts;
+  if (parts > 1) {
+    plan.parts = (int)parts;
+    plan.part_keys = (int)((max_k + parts - 1) / parts + 31) / 32 * 32;
+  }
+  return plan;
+}
+
+}  // namespace dare

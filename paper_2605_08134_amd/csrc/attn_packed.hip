@@ -1,0 +1,462 @@
+// Attention over packed sequences with shared key heads on the gfx950 matrix cores:
+//     out[t, h] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q[t, h] . k_j),   j < L(t)
+// over the keys of the token's own sequence, head h / G of K and V (G = query heads per key head).  L(t) is the number of
+// keys that the token sees: all of them, or those up to the end of its block of positions (attn_packed.h).
+//
+// Rows.  The G heads of a token read the same keys, so what a workgroup takes is rows (token, head of the group), head
+// fastest, of one key head: a key that is in LDS serves G times the tokens, and single tokens fill G rows of a matrix
+// instruction instead of one.  A row's keys are a prefix of its sequence, longer from token to token: a mask is needed
+// only where a row's last keys lie.
+//
+// Blocks.  How many rows a sequence has is known on the device only.  Sequence b gets the block numbers from
+// floor(rows in front of it / BM) + b on, which is never less than the blocks that it needs: a workgroup finds its
+// sequence by a search over q_off, no sum over the sequences in front of it, and the grid is at most a block per sequence
+// larger than a perfect one.  The last blocks start first: under a causal mask they are the longest.
+//
+// Logits are formed transposed, S^T = K Q^T, with v_mfma_f32_16x16x32_bf16: a lane holds logits of one row, and the
+// probabilities are in the layout of the second operand of O^T = V^T P^T, whose first operand is read from the row-major
+// V tile by the LDS transpose read.  Running maximum (its reference, in base 2) and sum per row in fp32; probabilities are
+// rounded to bf16 for the value product, as the matrix cores take them, and the sum is taken over them as rounded.
+//
+// Values in masked places do not count, whatever they are: a tile in which some row does not see some key multiplies with
+// those elements of V that are not finite replaced by 0, and adds what is not finite to the rows that see it.
+#include "attn_packed_rows.h"
+
+namespace dare {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct PackedDev {
+  const bf16_t* q;
+  const bf16_t* k;
+  const bf16_t* v;
+  bf16_t* out;
+  long ldq, ldk, ldv, ldo;
+  PackedRows rows;
+  int n_kv;
+  int max_parts;    // parts launched per block; with one part there is no workspace
+  int part_tiles;   // tiles of a part, at least
+  float* parts;     // [block][key head][part] partial results
+  float scale_log2;
+};
+
+typedef __attribute__((address_space(3))) void* lptr_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
+typedef const __attribute__((address_space(3))) bf16x8* lds_frag_t;
+typedef const __attribute__((address_space(3))) bf16_t* lds_elem_t;
+
+// ---- tiles in LDS ------------------------------------------------------------------------
+// Rows of K and V lie in LDS as in memory, 16-byte chunk c of key j at place c ^ swizzle(j): a K fragment (16 keys at one
+// chunk) and the transpose read of V (8 keys at 32 bytes at a time) meet no bank twice.  The swizzle of a key depends
+// on its place in a run of 16 only.
+template <int DH>
+__device__ __forceinline__ constexpr int k_swizzle(int key) {
+  return DH == 128 ? key & 15 : key >> 1 & 7;
+}
+template <int DH>
+__device__ __forceinline__ constexpr int v_swizzle(int key) {
+  return DH == 128 ? (key & 3) << 2 | (key >> 2 & 1) << 1 : (key >> 1 & 3) << 1;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// KEYS rows of K or V, from key `first` of the sequence on, to LDS address `to`, by one wave; rows from `len` on repeat
+// the last one.  Waited for by hand (a compiler that sees the load puts a wait for all of them in front of every transpose read).
+template <int DH, int KEYS, bool V>
+__device__ __forceinline__ void load_rows(const bf16_t* base, long ld, int first, int len, unsigned to) {
+  constexpr int CPR = DH / 8, RPL = 64 / CPR, N = KEYS / RPL;  // chunks per row, rows per load, loads
+  const int lane = threadIdx.x & 63;
+  const bf16_t* from = base + (long)first * ld;
+  const unsigned row_bytes = (unsigned)ld * 2;
+  const int end = len - 1 - first;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int key = i * RPL + lane / CPR;
+    const int chunk = (lane % CPR) ^ (V ? v_swizzle<DH>(key) : k_swizzle<DH>(key));
+    const unsigned at = (unsigned)(key < end ? key : end) * row_bytes + chunk * 16;
+    // (the LDS address is an operand in M0, set by the compiler; a wait state between the move to M0 and the load)
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(from), "{m0}"(to + i * 1024) : "memory");
+  }
+}
+
+// Maximum over the lanes L, L ^ 16, L ^ 32 and L ^ 48, which hold the same row
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// 32 keys against R blocks of 16 rows.  kt, vt: LDS addresses of the keys' rows; key0: number of the first one.
+// MASKED: row r of a lane sees keys below lim[r] only.
+template <int DH, int R>
+struct Rows {
+  static constexpr int CB = DH / 16;  // 16-channel blocks
+  bf16x8 qf[R][DH / 32];
+  f32x4 acc[CB][R];                   // channels 16 c + 4 kq .. + 3 of row l16
+  float m[R], l[R];                   // reference in base 2, this lane's part of the sum
+  int lim[R];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      m[r] = -__FLT_MAX__;
+      l[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // x[r][kb][e]: logit of key key0 + 16 kb + 4 kq + e
+  __device__ __forceinline__ void logits(unsigned kt, f32x4 (&x)[R][2]) const {
+    constexpr int ROWB = DH * 2;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) x[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < DH / 32; ++ks) {
+        const bf16x8 kf = *(lds_frag_t)(kt + (kb * 16 + l16) * ROWB + ((ks * 4 + kq) ^ k_swizzle<DH>(l16)) * 16);
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], x[r][kb], 0, 0, 0);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void mask(f32x4 (&x)[R][2], int key0) const {
+    const int kq = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+        if (key0 + (n >> 2) * 16 + kq * 4 + (n & 3) >= lim[r]) x[r][n >> 2][n & 3] = -INFINITY;
+  }
+
+  // The reference moves only when a maximum is 2^8 above it (any reference gives the same result up to rounding);
+  // it stays finite, so a row that sees nothing has probabilities 0.
+  __device__ __forceinline__ void softmax(const f32x4 (&x)[R][2], bf16x8 (&pf)[R], float scale_log2) {
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float top = x[r][0][0];
+#pragma unroll
+      for (int n = 1; n < 8; ++n) top = fmaxf(top, x[r][n >> 2][n & 3]);
+      top = row_max(top) * scale_log2;  // scale > 0
+      const bool grow = top > m[r] + 8.f;
+      if (__any(grow)) {
+        const float m_new = grow ? top : m[r], alpha = __builtin_amdgcn_exp2f(m[r] - m_new);
+        m[r] = m_new;
+        l[r] *= alpha;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[c][r] *= alpha;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int n = 0; n < 8; n += 2) {
+        f32x2 v;
+        v[0] = __builtin_amdgcn_exp2f(fmaf(x[r][n >> 2][n & 3], scale_log2, -m[r]));
+        v[1] = __builtin_amdgcn_exp2f(fmaf(x[r][n >> 2][(n & 3) + 1], scale_log2, -m[r]));
+        const bf16x2 pb = __builtin_convertvector(v, bf16x2);
+        sum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum, false);
+        pf[r][n] = pb[0];
+        pf[r][n + 1] = pb[1];
+      }
+      l[r] += sum;
+    }
+  }
+
+  // O^T += V^T P^T: slot s of a fragment is key 16 (s / 4) + 4 kq + s % 4
+  template <bool MASKED>
+  __device__ __forceinline__ void values(unsigned vt, const bf16x8 (&pf)[R], int key0, int len_k) {
+    constexpr int ROWB = DH * 2;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+    const int key = kq * 4 + (l16 >> 2);
+    const unsigned at = key * ROWB + ((l16 >> 1 & 1) ^ v_swizzle<DH>(key)) * 16 + (l16 & 1) * 8;
+    unsigned bad = 0;  // elements that are not finite: a bit of 0x80008000 each
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      const unsigned va = vt + (at ^ (c * 32));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(va));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(va + 16 * ROWB));
+      u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      if constexpr (MASKED) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned top = ((w[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponent of all ones
+          bad |= top;
+          w[i] &= ~((top >> 15) * 0xffffu);
+        }
+      }
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+      for (int r = 0; r < R; ++r) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], acc[c][r], 0, 0, 0);
+    }
+    if constexpr (MASKED) {
+      if (__builtin_expect(__any(bad != 0), 0)) add_not_finite(vt, key0, len_k);
+    }
+  }
+
+  // What is not finite among the values, to the rows that see it (their probability is above 0)
+  __device__ __forceinline__ void add_not_finite(unsigned vt, int key0, int len_k) {
+    constexpr int ROWB = DH * 2;
+    const int kq = (threadIdx.x & 63) >> 4;
+    for (int j = 0; j < 32 && key0 + j < len_k; ++j) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        const unsigned va = vt + j * ROWB + ((c * 2 + (kq >> 1)) ^ v_swizzle<DH>(j)) * 16 + (kq & 1) * 8;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = (float)((lds_elem_t)(va))[e];
+          if (fabsf(v) < INFINITY) continue;
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (key0 + j < lim[r]) acc[c][r][e] += v;
+        }
+      }
+    }
+  }
+};
+
+// This lane's rows: row j of the sequence is token j / G, head j % G of the group; those past the last one repeat it.
+template <int DH, int R>
+__device__ __forceinline__ void take_rows(const PackedDev& p, const Place& at, int kvh, int row0, Rows<DH, R>& w, long (&out_at)[R]) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    int j = row0 + r * 16 + l16;
+    j = at.row0 + (j < at.rows ? j : at.rows - 1);
+    const int i = (unsigned)j / (unsigned)p.rows.group, head = kvh * p.rows.group + (j - i * p.rows.group);
+    const bf16_t* row = p.q + (long)(at.q0 + i) * p.ldq + head * DH + kq * 8;
+#pragma unroll
+    for (int ks = 0; ks < DH / 32; ++ks) w.qf[r][ks] = *reinterpret_cast<const bf16x8*>(row + ks * 32);
+    out_at[r] = (long)(at.q0 + i) * p.ldo + head * DH;
+    w.lim[r] = packed_limit(i, at.shift, at.len_k, p.rows.causal_block);
+  }
+}
+__device__ __forceinline__ int parts_of(const PackedDev& p, int tiles) {
+  int n = (tiles + p.part_tiles - 1) / p.part_tiles;
+  n = n < p.max_parts ? n : p.max_parts;
+  return n > 1 ? n : 1;
+}
+template <int DH, int BM>
+__device__ __forceinline__ float* part_slot(const PackedDev& p, int g, int kvh, int part) {
+  return p.parts + ((long)(g * p.n_kv + kvh) * p.max_parts + part) * packed_slot_floats(DH, BM);
+}
+
+// ---- few rows: 16 R of them, four waves that share the keys -------------------------------------
+// Every wave takes every fourth tile of 32 keys through two stages of its own, so that the waves meet at the end only.
+constexpr int kFewWaves = 4, kFewKeys = 32;
+
+template <int DH, int R>
+__global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedDev p) {
+  constexpr int BM = 16 * R, CB = DH / 16, TILE = kFewKeys * DH * 2, STAGE = 2 * TILE, L = TILE / 1024;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kFewWaves * 2 * STAGE];
+  __shared__ float m_all[kFewWaves][R][16], l_all[kFewWaves][R][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, kq = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
+  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
+  Place at;
+  if (!find_block<BM>(p.rows, g, at)) return;
+
+  const int least = row_limit(p.rows, at, at.row0), most = row_limit(p.rows, at, at.row0 + at.rows - 1);
+  const int tiles = (most + kFewKeys - 1) / kFewKeys, n_parts = parts_of(p, tiles);
+  if (part >= n_parts) return;
+  const int first = (int)((long)tiles * part / n_parts), last = (int)((long)tiles * (part + 1) / n_parts);
+
+  Rows<DH, R> w;
+  long out_at[R];
+  take_rows(p, at, kvh, 0, w, out_at);
+  w.clear();
+  const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
+  const bf16_t* vbase = p.v + (long)at.k0 * p.ldv + kvh * DH;
+  const unsigned lds0 = (unsigned)(size_t)(lptr_t)smem + wave * 2 * STAGE;
+  auto load_k = [&](int t, int s) __attribute__((always_inline)) { load_rows<DH, kFewKeys, false>(kbase, p.ldk, t * kFewKeys, at.len_k, lds0 + s * STAGE); };
+  auto load_v = [&](int t, int s) __attribute__((always_inline)) { load_rows<DH, kFewKeys, true>(vbase, p.ldv, t * kFewKeys, at.len_k, lds0 + s * STAGE + TILE); };
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (the queries are there)
+  wait_vmcnt<0>();
+  int t = first + wave, s = 0;
+  if (t < last) {
+    load_k(t, 0);
+    load_v(t, 0);
+  }
+  if (t + kFewWaves < last) {
+    load_k(t + kFewWaves, 1);
+    load_v(t + kFewWaves, 1);
+  }
+  for (; t < last; t += kFewWaves, s ^= 1) {
+    const bool one = t + kFewWaves < last, two = t + 2 * kFewWaves < last;
+    const unsigned kt = lds0 + s * STAGE, vt = kt + TILE;
+    const int key0 = t * kFewKeys;
+    const bool masked = key0 + kFewKeys > least;
+    f32x4 x[R][2];
+    bf16x8 pf[R];
+    if (one) wait_vmcnt<3 * L>(); else wait_vmcnt<L>();
+    w.logits(kt, x);
+    wait_lds();
+    if (two) load_k(t + 2 * kFewWaves, s);
+    if (masked) w.mask(x, key0);
+    w.softmax(x, pf, p.scale_log2);
+    if (two) wait_vmcnt<3 * L>(); else if (one) wait_vmcnt<2 * L>(); else wait_vmcnt<0>();
+    if (masked) w.template values<true>(vt, pf, key0, at.len_k); else w.template values<false>(vt, pf, key0, at.len_k);
+    wait_lds();
+    if (two) load_v(t + 2 * kFewWaves, s);
+  }
+
+  // ---- the waves' results are joined in their order, a share of the channel blocks by each ----
+  float* mine = reinterpret_cast<float*>(smem + wave * 2 * STAGE);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float l = row_sum(w.l[r]);
+    if (kq == 0) {
+      m_all[wave][r][l16] = w.m[r];
+      l_all[wave][r][l16] = l;
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) reinterpret_cast<f32x4*>(mine)[(c * R + r) * 64 + lane] = w.acc[c][r];
+  }
+  __syncthreads();
+  constexpr int OWN = CB / kFewWaves;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float m = m_all[0][r][l16], l = 0.f, f[kFewWaves];
+#pragma unroll
+    for (int o = 1; o < kFewWaves; ++o) m = fmaxf(m, m_all[o][r][l16]);
+#pragma unroll
+    for (int o = 0; o < kFewWaves; ++o) {
+      f[o] = __builtin_amdgcn_exp2f(m_all[o][r][l16] - m);
+      l += l_all[o][r][l16] * f[o];
+    }
+    const int row = r * 16 + l16;
+    if (row >= at.rows) continue;
+    f32x4 sum[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const int c = wave * OWN + i;
+      sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int o = 0; o < kFewWaves; ++o)
+        sum[i] += reinterpret_cast<const f32x4*>(smem + o * 2 * STAGE)[(c * R + r) * 64 + lane] * f[o];
+    }
+    if (n_parts > 1) {
+      float* slot = part_slot<DH, BM>(p, g, kvh, part);
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) *reinterpret_cast<f32x4*>(slot + row * DH + (wave * OWN + i) * 16 + kq * 4) = sum[i];
+      if (wave == 0 && kq == 0) {
+        slot[BM * DH + row] = m;
+        slot[BM * DH + BM + row] = l;
+      }
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        bf16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[i][e] * inv);
+        *reinterpret_cast<bf16x4*>(p.out + out_at[r] + (wave * OWN + i) * 16 + kq * 4) = o;
+      }
+    }
+  }
+}
+
+// ---- parts of a row's keys, joined in their order: a wave per row --------------------------------
+template <int DH, int BM, int KEYS>
+__global__ void __launch_bounds__(256) attn_packed_join_kernel(PackedDev p) {
+  constexpr int PER = DH / 64;
+  typedef float vec_t __attribute__((ext_vector_type(PER)));
+  typedef __bf16 out_t __attribute__((ext_vector_type(PER)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
+  Place at;
+  if (!find_block<BM>(p.rows, g, at)) return;
+  const int most = row_limit(p.rows, at, at.row0 + at.rows - 1);
+  const int n_parts = parts_of(p, (most + KEYS - 1) / KEYS);
+  if (n_parts < 2) return;
+  const float* slot = part_slot<DH, BM>(p, g, kvh, 0);
+  constexpr long SLOT = packed_slot_floats(DH, BM);
+  for (int row = wave; row < at.rows; row += 4) {
+    // (kMaxParts is at most the lanes of a wave)
+    const float m_own = lane < n_parts ? slot[lane * SLOT + BM * DH + row] : -__FLT_MAX__;
+    float m = m_own;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float f_own = __builtin_amdgcn_exp2f(m_own - m);
+    const float l = wave_sum(lane < n_parts ? slot[lane * SLOT + BM * DH + BM + row] * f_own : 0.f);
+    vec_t sum;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[e] = 0.f;
+    for (int q = 0; q < n_parts; ++q) {
+      const float f = __shfl(f_own, q, 64);
+      sum += *reinterpret_cast<const vec_t*>(slot + q * SLOT + row * DH + lane * PER) * f;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int j = at.row0 + row, i = (unsigned)j / (unsigned)p.rows.group, head = kvh * p.rows.group + (j - i * p.rows.group);
+    out_t o;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = (bf16_t)(sum[e] * inv);
+    *reinterpret_cast<out_t*>(p.out + (long)(at.q0 + i) * p.ldo + head * DH + lane * PER) = o;
+  }
+}
+
+template <int DH, int R>
+hipError_t launch_few(PackedDev p, const PackedPlan& plan, hipStream_t s) {
+  const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
+  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R>), grid, dim3(kFewWaves * 64), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.parts == 1) return e;
+  hipLaunchKernelGGL((attn_packed_join_kernel<DH, 16 * R, kFewKeys>), dim3((unsigned)(plan.blocks * p.n_kv)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t launch_dh(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  if (plan.rows == 16) return launch_few<DH, 1>(p, plan, s);
+  return launch_few<DH, 2>(p, plan, s);
+}
+
+PackedPlan plan_of(const PackedArgs& a) {
+  return packed_plan(a.batch, a.total_q, a.max_q, a.max_k, a.n_heads / a.n_kv_heads, a.n_kv_heads);
+}
+
+}  // namespace
+
+size_t packed_workspace_floats(int dtype, const PackedArgs& a) {
+  if (dtype != DARE_BF16) return 0;
+  const PackedPlan plan = plan_of(a);
+  return plan.parts == 1 ? 0 : (size_t)plan.blocks * a.n_kv_heads * plan.parts * packed_slot_floats(a.head_dim, plan.rows);
+}
+
+hipError_t launch_attn_packed_bf16(const PackedArgs& a, hipStream_t s) {
+  const PackedPlan plan = plan_of(a);
+  PackedDev p;
+  p.q = static_cast<const bf16_t*>(a.q);
+  p.k = static_cast<const bf16_t*>(a.k);
+  p.v = static_cast<const bf16_t*>(a.v);
+  p.out = static_cast<bf16_t*>(a.out);
+  p.ldq = a.ldq;
+  p.ldk = a.ldk;
+  p.ldv = a.ldv;
+  p.ldo = a.ldo;
+  p.rows = packed_rows(a, plan.blocks);
+  p.n_kv = a.n_kv_heads;
+  p.max_parts = plan.parts;
+  p.part_tiles = plan.part_keys / kFewKeys;
+  p.parts = a.workspace;
+  p.scale_log2 = a.scale * kLog2e;
+  return a.head_dim == 128 ? launch_dh<128>(p, plan, s) : launch_dh<64>(p, plan, s);
+}
+
+}  // namespace dare

@@ -1,0 +1,70 @@
+// Rows of attention over packed sequences, for the kernels of both types: block numbers, sequences, keys (see
+// attn_packed.hip).
+#pragma once
+
+#include "attn_packed.h"
+#include "dare_common.h"
+
+namespace dare {
+
+struct PackedRows {
+  const int32_t* q_off;
+  const int32_t* k_begin;
+  const int32_t* k_end;
+  int batch, total_q, k_rows;
+  int group;         // query heads per key head
+  int causal_block;
+  int n_blocks;      // row blocks launched
+};
+
+inline PackedRows packed_rows(const PackedArgs& a, int n_blocks) {
+  return {a.q_off, a.k_begin, a.k_end, a.batch, a.total_q, a.k_rows, a.n_heads / a.n_kv_heads, a.causal_block, n_blocks};
+}
+
+struct Place {
+  int q0, k0;        // first query token and first key of the sequence
+  int len_k, shift;  // its keys; keys in front of the first query (len_k - len_q)
+  int row0, rows;    // rows of the block: row0 .. row0 + rows - 1 of the sequence's
+};
+
+// Block g of BM rows; false if it is empty.  All lanes of a wave call it; the result is the same in all of them.  Whatever the
+// offsets hold, rows lie in [0, total_q) and keys in [0, k_rows).
+template <int BM>
+__device__ __forceinline__ bool find_block(const PackedRows& p, const int g, Place& at) {
+  const int lane = threadIdx.x & 63;
+  auto offset = [&](int b) __attribute__((always_inline)) {
+    const int o = p.q_off[b];
+    return o < 0 ? 0 : o > p.total_q ? p.total_q : o;
+  };
+  int lo = 0, n = p.batch;
+  while (n > 1) {  // 64 candidates at a time
+    const int step = (n + 63) >> 6, b = lane * step;
+    const bool before = b < n && (int)((unsigned)(offset(lo + b) * p.group) / BM) + lo + b <= g;
+    const int count = __builtin_popcountll(__ballot(before));
+    if (count == 0) return false;
+    lo += (count - 1) * step;
+    n -= (count - 1) * step;
+    n = n < step ? n : step;
+  }
+  const int first = __builtin_amdgcn_readfirstlane(offset(lo)), end = __builtin_amdgcn_readfirstlane(offset(lo + 1));
+  const int len_q = end > first ? end - first : 0;
+  at.q0 = first;
+  at.row0 = (g - lo - (int)((unsigned)(first * p.group) / BM)) * BM;
+  const int rows = len_q * p.group - at.row0;
+  if (at.row0 < 0 || rows <= 0) return false;
+  at.rows = rows < BM ? rows : BM;
+  int begin = __builtin_amdgcn_readfirstlane(p.k_begin[lo]), stop = __builtin_amdgcn_readfirstlane(p.k_end[lo]);
+  begin = begin < 0 ? 0 : begin > p.k_rows ? p.k_rows : begin;
+  stop = stop > p.k_rows ? p.k_rows : stop;
+  at.k0 = begin;
+  at.len_k = stop > begin ? stop - begin : 0;
+  at.shift = at.len_k - len_q;
+  return true;
+}
+
+// Keys that row j of the sequence sees
+__device__ __forceinline__ int row_limit(const PackedRows& p, const Place& at, int j) {
+  return packed_limit((unsigned)j / (unsigned)p.group, at.shift, at.len_k, p.causal_block);
+}
+
+}  // namespace dare

@@ -1068,4 +1068,189 @@ dare_status dare_k_copy_rows(const void* src, void* dst, int n_rows, int row_byt
   return e == hipSuccess ? DARE_OK : DARE_ERR_HIP;
 }
 
+// ---- decoder layers with shared key heads ---------------------------------------------------
+
+namespace {
+dare_status refuse(const char* what) { return fail(nullptr, DARE_ERR_INVALID_ARG, what); }
+dare_status unsupported(const char* what) { return fail(nullptr, DARE_ERR_UNSUPPORTED, what); }
+dare_status launched(hipError_t e, const char* where) { return e == hipSuccess ? DARE_OK : fail_hip(nullptr, e, where); }
+// rows of ld elements lie on 16-byte boundaries
+bool aligned(int dtype, const void* p, long ld) {
+  return ((uintptr_t)p | (uintptr_t)(ld * (dtype == DARE_BF16 ? 2 : 4))) % 16 == 0;
+}
+constexpr long kMaxLd = 1l << 24;  // (32-bit offsets inside a tile of rows)
+}  // namespace
+
+dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, int n, int k, int m, const void* bias, int act,
+                          const void* residual, long ldr, void* out, long ldo, void* hip_stream) {
+  if (dtype != DARE_F32 && dtype != DARE_BF16) return refuse("unknown dtype");
+  if (m < 0 || n < 1 || k < 1) return refuse("size out of range");
+  if (act < DARE_ACT_NONE || act > DARE_ACT_GELU_TANH) return refuse("unknown activation");
+  if (n % 64 != 0 || k % 64 != 0) return unsupported("n and k must be multiples of 64");
+  if (m > 1 << 24 || n > 1 << 20) return unsupported("more than 2^24 rows or 2^20 columns");
+  if (m == 0) return DARE_OK;
+  if (!a || !wt || !out) return refuse("null pointer");
+  if (lda < k || ldo < n || (residual && ldr < n)) return refuse("ld below the width of a row");
+  if (lda > kMaxLd || ldo > kMaxLd || (residual && ldr > kMaxLd)) return unsupported("ld beyond 2^24");
+  if (!aligned(dtype, a, lda) || !aligned(dtype, out, ldo) || !aligned(dtype, wt, 0) || (bias && !aligned(dtype, bias, 0)) ||
+      (residual && !aligned(dtype, residual, ldr)))
+    return refuse("rows must lie on 16-byte boundaries");
+  if (residual == out && residual && ldr != ldo) return refuse("a residual in the place of the output has its ld");
+  GemmArgs g{};
+  g.a = a;
+  g.lda = (int)lda;
+  g.wt = wt;
+  g.n = n;
+  g.k = k;
+  g.m_max = m;
+  g.c[0] = out;
+  g.ldc = (int)ldo;
+  g.seg_n = n;
+  g.k_parts = 1;
+  g.linear = 1;
+  g.bias = bias;
+  g.residual = residual;
+  g.ldr = ldr;
+  g.act = act;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return launched(dtype == DARE_BF16 ? launch_gemm_bf16(g, s) : launch_gemm_f32(g, s), "dare_k_linear");
+}
+
+dare_status dare_k_rope(int dtype, int layout, int n_tokens, int head_dim, int rot_dim, const int32_t* pos, const double* freqs,
+                        float magnitude, const void* q, long ldq, void* q_out, long ldqo, int n_heads, const void* k, long ldk,
+                        void* k_out, long ldko, const void* v, long ldv, void* v_out, long ldvo, int n_kv_heads,
+                        const int32_t* rows, int out_rows, void* hip_stream) {
+  if (dtype != DARE_F32 && dtype != DARE_BF16) return refuse("unknown dtype");
+  if (layout != DARE_ROPE_HALF && layout != DARE_ROPE_PAIRS) return refuse("unknown layout");
+  if (n_tokens < 0 || !std::isfinite(magnitude)) return refuse("size or magnitude out of range");
+  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim) return refuse("rot_dim must be even, 2 .. head_dim");
+  if (head_dim < 8 || head_dim % 8 != 0 || head_dim > kRopeMaxDim) return unsupported("head_dim must be a multiple of 8 up to 256");
+  if (n_tokens == 0) return DARE_OK;
+  if (!pos || !freqs) return refuse("null pointer");
+  if ((uintptr_t)pos % 4 != 0 || (uintptr_t)freqs % 8 != 0) return refuse("pos or freqs not aligned");
+  RopeArgs r{};
+  const void* x[3] = {q, k, v};
+  void* out[3] = {q_out, k_out, v_out};
+  const long ldx[3] = {ldq, ldk, ldv}, ldo[3] = {ldqo, ldko, ldvo};
+  const size_t esize = dtype == DARE_BF16 ? 2 : 4;
+  for (int i = 0; i < 3; ++i) {
+    if ((x[i] == nullptr) != (out[i] == nullptr)) return refuse("an input without its output, or the other way round");
+    if (!x[i]) continue;
+    const int heads = i == 0 ? n_heads : n_kv_heads;
+    if (heads < 1 || heads > 65535) return refuse("number of heads out of range");
+    if (ldx[i] < (long)heads * head_dim || ldo[i] < (long)heads * head_dim) return refuse("ld below the width of a row");
+    if (ldx[i] > kMaxLd || ldo[i] > kMaxLd) return unsupported("ld beyond 2^24");
+    if (((uintptr_t)x[i] | (uintptr_t)out[i]) % esize != 0) return refuse("tensors not aligned to their elements");
+    if (x[i] == out[i] && (ldx[i] != ldo[i] || (i > 0 && rows))) return refuse("in place: the same ld, and no rows");
+    r.x[i] = x[i];
+    r.out[i] = out[i];
+    r.ldx[i] = ldx[i];
+    r.ldo[i] = ldo[i];
+    r.heads[i] = heads;
+  }
+  if (rows && out_rows < 1) return refuse("rows without rows to write");
+  r.n = n_tokens;
+  r.dim = head_dim;
+  r.rot = rot_dim;
+  r.pairs = layout == DARE_ROPE_PAIRS;
+  r.pos = pos;
+  r.freqs = freqs;
+  r.rows = rows;
+  r.out_rows = out_rows;
+  r.magnitude = magnitude;
+  return launched(launch_rope(dtype, r, static_cast<hipStream_t>(hip_stream)), "dare_k_rope");
+}
+
+dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scaling, double factor, double context, double low,
+                              double high) {
+  if (!freqs) return refuse("null pointer");
+  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > kRopeMaxDim) return refuse("rot_dim must be even, 2 .. 256");
+  if (!(base > 0.0) || !std::isfinite(base)) return refuse("base must be above 0");
+  if (scaling < DARE_ROPE_SCALE_NONE || scaling > DARE_ROPE_SCALE_TURNS) return refuse("unknown scaling");
+  if (scaling != DARE_ROPE_SCALE_NONE && (!(factor > 0.0) || !std::isfinite(factor))) return refuse("factor must be above 0");
+  if (scaling == DARE_ROPE_SCALE_BASE && rot_dim < 4) return refuse("a stretched base needs two pairs");
+  if (scaling == DARE_ROPE_SCALE_TURNS && (!(context > 0.0) || !std::isfinite(context) || !(high > low) || !std::isfinite(high - low)))
+    return refuse("scaling by turns needs a context above 0 and high above low");
+  double host[kRopeMaxDim / 2];
+  if (scaling == DARE_ROPE_SCALE_BASE) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot_dim);
+    if (scaling == DARE_ROPE_SCALE_LINEAR) f /= factor;
+    if (scaling == DARE_ROPE_SCALE_TURNS) {
+      const double turns = context * f / 6.283185307179586476925, t = (turns - low) / (high - low);
+      const double g = t < 0.0 ? 0.0 : t > 1.0 ? 1.0 : t;
+      f *= g + (1.0 - g) / factor;
+    }
+    host[i] = f;
+  }
+  return launched(hipMemcpy(freqs, host, rot_dim / 2 * sizeof(double), hipMemcpyHostToDevice), "hipMemcpy");
+}
+
+namespace {
+dare_status check_packed(const dare_packed_config* c, PackedArgs* a) {
+  if (!c || c->struct_size != sizeof(dare_packed_config)) return refuse("null config, or struct_size does not match this library");
+  if (c->dtype != DARE_F32 && c->dtype != DARE_BF16) return refuse("unknown dtype");
+  if (c->batch < 0 || c->total_q < 0 || c->k_rows < 0 || c->max_q < 0 || c->max_k < 0 || c->causal_block < 0)
+    return refuse("negative size");
+  if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads != 0)
+    return refuse("n_heads must be a multiple of n_kv_heads");
+  if (!(c->scale > 0.f) || !std::isfinite(c->scale)) return refuse("scale must be above 0");
+  if (c->head_dim != 64 && c->head_dim != 128) return unsupported("head_dim must be 64 or 128");
+  const long wq = (long)c->n_heads * c->head_dim, wk = (long)c->n_kv_heads * c->head_dim;
+  if (c->ldq < wq || c->ldo < wq || c->ldk < wk || c->ldv < wk) return refuse("ld below the width of a row");
+  if (c->ldq > kMaxLd || c->ldo > kMaxLd || c->ldk > kMaxLd || c->ldv > kMaxLd) return unsupported("ld beyond 2^24");
+  if ((long)c->total_q * c->n_heads + 128l * c->batch >= 1l << 31) return unsupported("more than 2^31 query rows");
+  a->ldq = c->ldq;
+  a->ldk = c->ldk;
+  a->ldv = c->ldv;
+  a->ldo = c->ldo;
+  a->batch = c->batch;
+  a->total_q = c->total_q;
+  a->k_rows = c->k_rows;
+  a->max_q = c->max_q;
+  a->max_k = c->max_k;
+  a->n_heads = c->n_heads;
+  a->n_kv_heads = c->n_kv_heads;
+  a->head_dim = c->head_dim;
+  a->causal_block = c->causal_block;
+  a->scale = c->scale;
+  return DARE_OK;
+}
+}  // namespace
+
+dare_status dare_k_attention_packed_workspace(const dare_packed_config* cfg, size_t* bytes) {
+  if (!bytes) return refuse("null pointer");
+  PackedArgs a{};
+  const dare_status st = check_packed(cfg, &a);
+  *bytes = st == DARE_OK && a.batch > 0 && a.total_q > 0 ? packed_workspace_floats(cfg->dtype, a) * sizeof(float) : 0;
+  return st;
+}
+
+dare_status dare_k_attention_packed(const dare_packed_config* cfg, const void* q, const void* k, const void* v, void* out,
+                                    const int32_t* q_off, const int32_t* k_begin, const int32_t* k_end, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream) {
+  PackedArgs a{};
+  const dare_status st = check_packed(cfg, &a);
+  if (st != DARE_OK) return st;
+  if (a.batch == 0 || a.total_q == 0) return DARE_OK;
+  if (!q || !out || !q_off || !k_begin || !k_end || (a.k_rows > 0 && (!k || !v))) return refuse("null pointer");
+  if (!aligned(cfg->dtype, q, a.ldq) || !aligned(cfg->dtype, out, a.ldo) || !aligned(cfg->dtype, k, a.ldk) ||
+      !aligned(cfg->dtype, v, a.ldv))
+    return refuse("rows must lie on 16-byte boundaries");
+  if (((uintptr_t)q_off | (uintptr_t)k_begin | (uintptr_t)k_end) % 4 != 0) return refuse("offsets not aligned");
+  const size_t need = packed_workspace_floats(cfg->dtype, a) * sizeof(float);
+  if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
+    return refuse("workspace missing, too small or not on a 16-byte boundary");
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.q_off = q_off;
+  a.k_begin = k_begin;
+  a.k_end = k_end;
+  a.workspace = static_cast<float*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return launched(cfg->dtype == DARE_BF16 ? launch_attn_packed_bf16(a, s) : launch_attn_packed_f32(a, s), "dare_k_attention_packed");
+}
+
 }  // extern "C"

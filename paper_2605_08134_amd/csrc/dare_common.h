@@ -79,6 +79,13 @@ struct GemmArgs {
   int part_n;
   const int32_t* part_idx;
   const int32_t* part_m_dev;
+  // 1: c[0] = act(product + bias) + residual (all rows, one segment, nothing else of the above).  bias [n], residual
+  // [*, ldr] of the type, either of them optional; act a DARE_ACT_*
+  int linear;
+  const void* bias;
+  const void* residual;
+  long ldr;
+  int act;
 };
 constexpr int kSelMaxTokens = 2048, kSelMaxTokensF32 = 1024;
 constexpr size_t gemm_split_tiles_bytes() { return (size_t)kSplitTiles * 2 * kPpRows * 128 * sizeof(float); }
@@ -154,6 +161,41 @@ constexpr int kAttnParts = 256;  // parts of a launch, at most: one per CU
 constexpr size_t attn_parts_elems(int head_dim) { return (size_t)kAttnParts * 64 * 2 * (head_dim / 2 + 2); }
 hipError_t launch_attn_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t s);
+
+struct RopeArgs {
+  const void* x[3];  // q, k, v or nullptr
+  void* out[3];
+  long ldx[3], ldo[3];
+  int heads[3];
+  int n, dim, rot;
+  bool pairs;
+  const int32_t* pos;
+  const double* freqs;
+  const int32_t* rows;  // rows of the k and v outputs, or nullptr: the tokens'
+  int out_rows;
+  float magnitude;
+};
+constexpr int kRopeMaxDim = 256;
+hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s);
+
+// Attention over packed sequences (dare_k_attention_packed)
+struct PackedArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  long ldq, ldk, ldv, ldo;
+  const int32_t* q_off;
+  const int32_t* k_begin;
+  const int32_t* k_end;
+  int batch, total_q, k_rows, max_q, max_k;
+  int n_heads, n_kv_heads, head_dim, causal_block;
+  float scale;
+  float* workspace;  // packed_workspace_floats() of it
+};
+size_t packed_workspace_floats(int dtype, const PackedArgs& a);
+hipError_t launch_attn_packed_bf16(const PackedArgs& a, hipStream_t s);
+hipError_t launch_attn_packed_f32(const PackedArgs& a, hipStream_t s);
 
 hipError_t launch_pack_weight(int dtype, const void* w, int rows_k, int cols_n, void* wt,
                               int ldwt, hipStream_t s);

@@ -78,6 +78,11 @@ struct GemmDev {
   int part_n;
   const int32_t* part_idx;
   const int32_t* part_m_dev;
+  // act(product + bias) + residual (LINEAR forms of the tiles)
+  const bf16_t* bias;
+  const bf16_t* residual;
+  long ldr;
+  int act;
 };
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
@@ -142,6 +147,66 @@ __device__ __forceinline__ float silu(float g) {
   const float scale = SCALED && g < kGateLow ? 0x1p-32f : 1.0f;
   const float d = fmaf(__expf(-g), scale, scale), r = __builtin_amdgcn_rcpf(d), q = g * r;
   return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-d, q, g), r, q) * scale, d, g);
+}
+
+// Activation of N values at once: what it is is settled outside the loop.  Reciprocals and exponentials by the hardware's
+// instructions, 1 ulp of fp32 each, behind them a rounding to bf16.
+// GELU: z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt(2)) / 2 with erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2), t = 1 / (1 + p x)
+// (Abramowitz and Stegun, 7.1.26), 1.5e-7 off at most: a sixth of the instructions of a full erfc.
+// Tanh form: z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
+template <int N>
+__device__ __forceinline__ void activate(const int act, float (&v)[N]) {
+  if (act == DARE_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * v[i]));
+  } else if (act == DARE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = v[i], x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+      float e = fmaf(t, 1.061405429f, -1.453152027f);
+      e = fmaf(t, e, 1.421413741f);
+      e = fmaf(t, e, -0.284496736f);
+      e = fmaf(t, e, 0.254829592f) * t * __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+      v[i] = fmaf(-0.5f * fabsf(z), e, fmaxf(z, 0.f));
+    }
+  } else if (act == DARE_ACT_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float z = v[i];
+      v[i] = z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.30220819f * fmaf(0.044715f * z * z, z, z)));
+    }
+  }
+}
+
+// The same with act(product + bias) + residual in the place of what it describes: sums, activation and residual sum in fp32, one rounding.
+// The residual's rows may be the output's: a lane reads what it stores.
+template <int W, int TM, int TN, class Value>
+__device__ __forceinline__ void store_linear(const GemmDev& p, const int (&tok)[TM], const bool (&live)[TM],
+                                             const int (&col)[TN], Value value) {
+  typedef __bf16 out_t __attribute__((ext_vector_type(W)));
+  const long ldc = p.ldc, ldr = p.ldr;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int c = col[j];
+    if (c >= p.n) continue;
+    out_t res[TM], bias;
+    if (p.residual) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) res[i] = *reinterpret_cast<const out_t*>(p.residual + tok[i] * ldr + c);
+    }
+    if (p.bias) bias = *reinterpret_cast<const out_t*>(p.bias + c);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      float v[W];
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] = value(i, j, e) + (p.bias ? (float)bias[e] : 0.f);
+      activate(p.act, v);
+      out_t o;
+#pragma unroll
+      for (int e = 0; e < W; ++e) o[e] = (bf16_t)(v[e] + (p.residual ? (float)res[i][e] : 0.f));
+      if (live[i]) *reinterpret_cast<out_t*>(reinterpret_cast<bf16_t*>(p.c0) + tok[i] * ldc + c) = o;
+    }
+  }
 }
 
 // Epilogue of a wave tile: W (4 or 8) neighbouring output columns col[j] .. col[j] + W - 1 (col[j] a multiple
@@ -431,7 +496,7 @@ __device__ __forceinline__ void gemm_tile(const GemmDev& p, const int m, unsigne
 // summed 16, results differ from then by single bf16 roundings.)  The k of a k-step halved
 // between two groups of four waves with twice the wave tile (half the fragment reads) is no faster.
 // Some waves repeat the last group of rows (128 x 96: 32 loads for 28 groups).
-template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, bool LINEAR = false>
 __device__ __forceinline__ bool gemm_tile16(const GemmDev& p, const int m, unsigned char* smem, const int tid,
                                             const int vblock, lds_idx_t lidx = nullptr,
                                             const int forced_tile_m = -1, const int forced_tile_n = 0) {
@@ -612,8 +677,11 @@ __device__ __forceinline__ bool gemm_tile16(const GemmDev& p, const int m, unsig
   int col[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j) col[j] = n0 + wave_n * WN + j * 16 + kq * 4;
-  store_tile<4>(p, p.c32, tok_out, live_out, col,
-                [&](int i, int j, int e) __attribute__((always_inline)) { return acc[i][j][e]; });
+  auto value = [&](int i, int j, int e) __attribute__((always_inline)) { return acc[i][j][e]; };
+  if constexpr (LINEAR)
+    store_linear<4>(p, tok_out, live_out, col, value);
+  else
+    store_tile<4>(p, p.c32, tok_out, live_out, col, value);
   return true;
 }
 
@@ -660,7 +728,7 @@ constexpr int pp_smem_bytes() {
 __device__ __forceinline__ int pp_bkey(int r) { return ((r >> 1) & 1) | (((r >> 3) & 3) << 1); }
 
 // vblock, lidx and the result as in gemm_tile16; called by all 512 threads.
-template <int TN, bool SPLIT = false>
+template <int TN, bool SPLIT = false, bool LINEAR = false>
 __device__ __forceinline__ bool gemm_tile_pp(const GemmDev& p, const int m, unsigned char* smem, const int vblock,
                                              lds_idx_t lidx = nullptr) {
   static_assert(TN >= 2 && TN <= 4, "column blocks of 32 per wave");
@@ -945,9 +1013,11 @@ __device__ __forceinline__ bool gemm_tile_pp(const GemmDev& p, const int m, unsi
   int col[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j) col[j] = n0 + grp * (32 * TN) + j * 32 + kq * 8;
-  store_tile<8>(p, p.c32, tok_out, live_out, col, [&](int i, int j, int e) __attribute__((always_inline)) {
-    return acc[i][j * 2 + (e >> 2)][e & 3];
-  });
+  auto value = [&](int i, int j, int e) __attribute__((always_inline)) { return acc[i][j * 2 + (e >> 2)][e & 3]; };
+  if constexpr (LINEAR)
+    store_linear<8>(p, tok_out, live_out, col, value);
+  else
+    store_tile<8>(p, p.c32, tok_out, live_out, col, value);
   return true;
 }
 
@@ -999,7 +1069,8 @@ __device__ __forceinline__ void store16(bf16_t* to, const u32x4 v) {
 // The tiles blockIdx.x, blockIdx.x + gridDim.x, ..; called by all 256 threads.  k of kQuadMinSteps k-steps or more (loads two ahead, and
 // the first one's zero sums).
 // PART: the columns from part_n on for all rows, those in front of it for the part_m rows of the second list.
-template <int TN, bool STREAM, bool PART = false>
+// LINEAR: act(sums + bias) + residual.
+template <int TN, bool STREAM, bool PART = false, bool LINEAR = false>
 __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, unsigned char* smem, const int part_m = 0) {
   static_assert(TN == 3 || TN == 4, "column blocks of 32 per wave");
   constexpr int BM = kPpRows, BN = 64 * TN;
@@ -1198,7 +1269,7 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
     };
     // acc[i][2 j + h][e] = C[row, col], row = m0 + 128 wm + 16 i + l16, col = col0 + 32 j + 8 kq + 4 h + e
     const bool low = l16 < 8;
-    if (!PART && p.swiglu_pairs) {
+    if (!PART && !LINEAR && p.swiglu_pairs) {
       const long ldc = p.ldc;
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
@@ -1260,7 +1331,45 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
         }
       }
     } else {
-      if (!PART && p.c32 && col0 < p.c32_cols) {
+      if constexpr (LINEAR) {
+        // (the residual's rows a row of the tile ahead; columns behind the last one read the last ones, nobody stores them)
+        bf16x8 bias[TN], res[2][TN];
+        int at_col[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int c = col0 + j * 32 + kq * 8;
+          at_col[j] = c < n_end ? c : n_end - 8;
+          if (p.bias) bias[j] = *reinterpret_cast<const bf16x8*>(p.bias + at_col[j]);
+        }
+        auto residual = [&](int i) __attribute__((always_inline)) {
+          const bf16_t* row = p.residual + tok[i] * p.ldr;
+#pragma unroll
+          for (int j = 0; j < TN; ++j) res[i & 1][j] = *reinterpret_cast<const bf16x8*>(row + at_col[j]);
+        };
+        if (p.residual) residual(0);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+          if (p.residual && i + 1 < NA) residual(i + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = value(i, j, e) + (p.bias ? (float)bias[j][e] : 0.f);
+            activate(p.act, v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              f32x4 sum;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum[e] = v[4 * h + e] + (p.residual ? (float)res[i & 1][j][4 * h + e] : 0.f);
+              acc[i][2 * j + h] = sum;
+              asm volatile("" : "+a"(acc[i][2 * j + h]));
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (!PART && !LINEAR && p.c32 && col0 < p.c32_cols) {
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -1272,7 +1381,7 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
             if (live[i] && c < p.c32_cols) *reinterpret_cast<f32x4*>(p.c32 + (long)tok[i] * p.c32_cols + c) = v;
           }
       }
-      if (p.rope && col0 < p.rope_cols) {
+      if (!LINEAR && p.rope && col0 < p.rope_cols) {
         // (the table's rows a row of the tile ahead of their use; columns that are not rotated read one that is)
         f32x4 cs[2][NB];
         auto table = [&](int i) __attribute__((always_inline)) {
@@ -1377,7 +1486,7 @@ __global__ void __launch_bounds__(256, 1) gemm_bf16_quad_kernel(GemmDev p) {
 // only), 16 k-steps of 32 in flight per wave (8 with two row blocks), multiply with v_mfma_f32_16x16x32_bf16
 // (weight fragment first, so a lane again owns one row and four neighbouring columns), and
 // the partial sums of the waves are added in wave order through LDS.
-template <int NW, int TMS>
+template <int NW, int TMS, bool LINEAR = false>
 __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsigned char* smem, const int tid,
                                             lds_idx_t lidx = nullptr) {
   constexpr int UNR = TMS == 1 ? 16 : 8;
@@ -1442,8 +1551,11 @@ __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsig
         for (int w = 1; w < NW; ++w) acc[t] += red[(w * TMS + t) * 64 + lane];
       }
       const int col[1] = {n0 + kq * 4};
-      store_tile<4>(p, p.c32, tok, live, col,
-                    [&](int t, int, int e) __attribute__((always_inline)) { return acc[t][e]; });
+      auto value = [&](int t, int, int e) __attribute__((always_inline)) { return acc[t][e]; };
+      if constexpr (LINEAR)
+        store_linear<4>(p, tok, live, col, value);
+      else
+        store_tile<4>(p, p.c32, tok, live, col, value);
     }
     __syncthreads();
   }
@@ -1470,6 +1582,28 @@ template <int TN, bool SPLIT>
 __global__ void __launch_bounds__(512) gemm_bf16_pp_kernel(GemmDev p) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[pp_smem_bytes<TN>()];
   gemm_tile_pp<TN, SPLIT>(p, p.m_max, smem, blockIdx.x);
+}
+
+// ---- act(A W + bias) + residual of all rows ---------------------------------------------------
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ void __launch_bounds__(512) linear_bf16_tile16_kernel(GemmDev p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[smem_bytes<BM, BN, STAGES>()];
+  gemm_tile16<BM, BN, WAVES_M, WAVES_N, STAGES, true>(p, p.m_max, smem, threadIdx.x, blockIdx.x);
+}
+template <int TN>
+__global__ void __launch_bounds__(512) linear_bf16_pp_kernel(GemmDev p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[pp_smem_bytes<TN>()];
+  gemm_tile_pp<TN, false, true>(p, p.m_max, smem, blockIdx.x);
+}
+template <int TN, bool STREAM>
+__global__ void __launch_bounds__(256, 1) linear_bf16_quad_kernel(GemmDev p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kQuadSmem];
+  gemm_tiles_quad<TN, STREAM, false, true>(p, p.m_max, smem);
+}
+template <int TMS>
+__global__ void __launch_bounds__(512) linear_bf16_skinny_kernel(GemmDev p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[8 * TMS * 64 * 16];
+  skinny_tile<8, TMS, true>(p, p.m_max, smem, threadIdx.x);
 }
 
 // ---- row count read on the device: the tile shape follows it -------------------------
@@ -1947,6 +2081,10 @@ GemmDev to_dev(const GemmArgs& g) {
   p.part_n = g.part_n;
   p.part_idx = g.part_idx;
   p.part_m_dev = g.part_m_dev;
+  p.bias = static_cast<const bf16_t*>(g.bias);
+  p.residual = static_cast<const bf16_t*>(g.residual);
+  p.ldr = g.ldr;
+  p.act = g.act;
   return p;
 }
 
@@ -2014,6 +2152,53 @@ hipError_t launch_rows_wide(const GemmArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The shapes of the plain projection by its rule, and the stream over the weights for few rows of narrow outputs
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+hipError_t launch_linear_tile16(const GemmArgs& g, hipStream_t s) {
+  hipLaunchKernelGGL((linear_bf16_tile16_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>),
+                     dim3(grid_for(tiles_of(g.m_max, g.n, BM, BN))), dim3(512), 0, s, to_dev(g));
+  return hipGetLastError();
+}
+template <int TN>
+hipError_t launch_linear_pp(const GemmArgs& g, hipStream_t s) {
+  hipLaunchKernelGGL(linear_bf16_pp_kernel<TN>, dim3(grid_for(tiles_of(g.m_max, g.n, kPpRows, 64 * TN))), dim3(512), 0, s,
+                     to_dev(g));
+  return hipGetLastError();
+}
+template <int TN>
+hipError_t launch_linear_quad(const GemmArgs& g, hipStream_t s) {
+  const int tiles = grid_for(tiles_of(g.m_max, g.n, kPpRows, 64 * TN));
+  const dim3 grid(tiles < kWideGrid ? tiles : kWideGrid);
+  if (TN == 4 && (long)g.m_max * g.n * 2 > kStreamBytes)
+    hipLaunchKernelGGL((linear_bf16_quad_kernel<TN, TN == 4>), grid, dim3(256), 0, s, to_dev(g));
+  else
+    hipLaunchKernelGGL((linear_bf16_quad_kernel<TN, false>), grid, dim3(256), 0, s, to_dev(g));
+  return hipGetLastError();
+}
+hipError_t launch_linear(const GemmArgs& g, hipStream_t s) {
+  if (g.m_max <= kSkinnyRows && g.n < kSkinnyMaxN) {
+    if (g.m_max <= 16)
+      hipLaunchKernelGGL(linear_bf16_skinny_kernel<1>, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
+    else
+      hipLaunchKernelGGL(linear_bf16_skinny_kernel<2>, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
+    return hipGetLastError();
+  }
+  switch (gemm_route(g.m_max, g.n, g.k, 1, false)) {
+    case GemmRoute::kQuad256: return launch_linear_quad<4>(g, s);
+    case GemmRoute::kQuad192: return launch_linear_quad<3>(g, s);
+    case GemmRoute::kPp256: return launch_linear_pp<4>(g, s);
+    case GemmRoute::kPp192: return launch_linear_pp<3>(g, s);
+    case GemmRoute::kPp128: return launch_linear_pp<2>(g, s);
+    case GemmRoute::k128x192: return launch_linear_tile16<128, 192, 2, 4, 3>(g, s);
+    case GemmRoute::k128x128: return launch_linear_tile16<128, 128, 2, 4, 4>(g, s);
+    case GemmRoute::k128x96: return launch_linear_tile16<128, 96, 4, 2, 4>(g, s);
+    case GemmRoute::k64x128: return launch_linear_tile16<64, 128, 2, 4, 5>(g, s);
+    case GemmRoute::k64x96: return launch_linear_tile16<64, 96, 4, 2, 6>(g, s);
+    case GemmRoute::k64x64: return launch_linear_tile16<64, 64, 2, 4, 8>(g, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& g, hipStream_t s) {
@@ -2027,6 +2212,7 @@ hipError_t launch_gemm_bf16(const GemmArgs& g, hipStream_t s) {
   }
   if (g.m_dev || g.sel_mask) return launch_rows_wide(g, s);
   if (g.m_max == 0) return hipSuccess;
+  if (g.linear) return launch_linear(g, s);
   switch (gemm_route(g.m_max, g.n, g.k, g.k_parts, g.split_tiles && !g.c32)) {
     case GemmRoute::kPp128Split: return launch_pp<2, true>(g, s);
     case GemmRoute::kQuad256: return launch_quad<4>(g, s);

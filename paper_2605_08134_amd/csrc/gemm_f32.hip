@@ -41,7 +41,26 @@ struct GemmF32Dev {
   int32_t* sel_idx_out2;
   int32_t* sel_off_out;
   int32_t* sel_count_out;
+  const float* bias;        // act(product + bias) + residual (the LINEAR form)
+  const float* residual;
+  long ldr;
+  int act;
 };
+
+// silu(z) = z / (1 + e^-z); gelu(z) = z Phi(z) = z erfc(-z / sqrt(2)) / 2; its tanh form z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float activate_f32(int act, float z) {
+  if (act == DARE_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == DARE_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
+  if (act == DARE_ACT_GELU_TANH) return z / (1.f + expf(-1.59576912f * fmaf(0.044715f * z * z, z, z)));
+  return z;
+}
+__device__ __forceinline__ void store4_linear_f32(const GemmF32Dev& p, long tok, int col, f32x4 v) {
+  if (p.bias) v += *reinterpret_cast<const f32x4*>(p.bias + col);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = activate_f32(p.act, v[e]);
+  if (p.residual) v += *reinterpret_cast<const f32x4*>(p.residual + tok * p.ldr + col);
+  *reinterpret_cast<f32x4*>(p.c0 + tok * p.ldc + col) = v;
+}
 
 // four neighbouring output columns col .. col + 3 (col a multiple of 4) of token tok
 __device__ __forceinline__ void store4_f32(const GemmF32Dev& p, long tok, int col, f32x4 v) {
@@ -121,7 +140,7 @@ constexpr int kKParts = 4;  // quarters of k (k is a multiple of 64: whole steps
 // Four waves on one tile of 16 TM x 16 TN, a quarter of k each, sums added through LDS.  UNR: steps of 16 k
 // whose loads are in flight at once (registers allow one for 64 x 64, whose 64 MFMAs per step
 // cover a load).
-template <int TM, int TN, int UNR, bool FUSED>
+template <int TM, int TN, int UNR, bool FUSED, bool LINEAR = false>
 __global__ void __launch_bounds__(256) gemm_f32_kernel(GemmF32Dev p) {
   constexpr int BM = 16 * TM, BN = 16 * TN;
   __shared__ f32x4 part_sum[kKParts][TM * TN][64];
@@ -209,16 +228,23 @@ __global__ void __launch_bounds__(256) gemm_f32_kernel(GemmF32Dev p) {
 #pragma unroll
     for (int w = 1; w < kKParts; ++w) v += part_sum[w][t][lane];
     const int row = m0 + i * 16 + l16, col = n0 + j * 16 + kq * 4;
-    if (row < m && col < p.n) store4_f32(p, tok[i], col, v);
+    if (row < m && col < p.n) {
+      if constexpr (LINEAR)
+        store4_linear_f32(p, tok[i], col, v);
+      else
+        store4_f32(p, tok[i], col, v);
+    }
   }
 }
 
 template <int TM, int TN, int UNR>
-hipError_t launch_shape(const GemmF32Dev& p, hipStream_t s) {
+hipError_t launch_shape(const GemmF32Dev& p, bool linear, hipStream_t s) {
   constexpr int BM = 16 * TM, BN = 16 * TN;
   const int tm = (p.m_max + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
   if (tm == 0 || tn == 0) return hipSuccess;
-  if (p.sel_mask)
+  if (linear)
+    hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, false, true>), dim3(tm, tn), dim3(256), 0, s, p);
+  else if (p.sel_mask)
     hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, true>), dim3(tm, tn), dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, false>), dim3(tm, tn), dim3(256), 0, s, p);
@@ -255,6 +281,10 @@ hipError_t launch_gemm_f32(const GemmArgs& g, hipStream_t s) {
   p.sel_idx_out2 = g.sel_idx_out2;
   p.sel_off_out = g.sel_off_out;
   p.sel_count_out = g.sel_count_out;
+  p.bias = static_cast<const float*>(g.bias);
+  p.residual = static_cast<const float*>(g.residual);
+  p.ldr = g.ldr;
+  p.act = g.act;
   if (p.sel_mask && (long)g.sel_batch * g.sel_seq > kSelMaxTokensF32) return hipErrorInvalidValue;
   // The largest tile that gives most of the chip's 256 CUs a workgroup.  Measured (us; before: 64 x 64
   // tiles through LDS): 1024 x 12288 x 4096 1325 -> 880, 1024 x 2048 x 2048 141 -> 80 and
@@ -262,9 +292,9 @@ hipError_t launch_gemm_f32(const GemmArgs& g, hipStream_t s) {
   // 925 (64 x 64), 64 x 4096 x 4096 235 -> 43 (32 x 32; 64 with 16 x 16, 84 with 64 x 64).
   auto tiles = [&](int b) { return (long)((g.m_max + b - 1) / b) * ((g.n + b - 1) / b); };
   constexpr long kFill = 192;
-  if (tiles(64) >= kFill) return launch_shape<4, 4, 1>(p, s);
-  if (tiles(32) >= kFill) return launch_shape<2, 2, 4>(p, s);
-  return launch_shape<1, 1, 4>(p, s);
+  if (tiles(64) >= kFill) return launch_shape<4, 4, 1>(p, g.linear, s);
+  if (tiles(32) >= kFill) return launch_shape<2, 2, 4>(p, g.linear, s);
+  return launch_shape<1, 1, 4>(p, g.linear, s);
 }
 
 }  // namespace dare
