@@ -29,18 +29,18 @@ struct PackedPlan {
 
 constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, int group, int n_kv) {
   PackedPlan plan{};
-  plan.rows = (long)max_q * group <= 16 ? 16 : 32;
+  plan.rows = (long)max_q * group <= 16 ? 16 : (long)max_q * group <= 32 ? 32 : 128;
   plan.blocks = (int)((long)total_q * group / plan.rows) + batch;
   plan.parts = 1;
   plan.part_keys = 1 << 30;
   // As many parts as fill the 256 CUs about three times, of 256 keys at least
   const long pairs = (long)plan.blocks * n_kv;
-  long parts = 768 / (pairs > 0 ? pairs : 1);
+  long parts = (plan.rows == 128 ? 512 : 768) / (pairs > 0 ? pairs : 1);
   if (parts > max_k / 256) parts = max_k / 256;
   if (parts > kPackedMaxParts) parts = kPackedMaxParts;
   if (parts > 1) {
     plan.parts = (int)parts;
-    plan.part_keys = (int)((max_k + parts - 1) / parts + 31) / 32 * 32;
+    plan.part_keys = (int)((max_k + parts - 1) / parts + 63) / 64 * 64;
   }
   return plan;
 }

@@ -20,6 +20,8 @@
 //
 // Values in masked places do not count, whatever they are: a tile in which some row does not see some key multiplies with
 // those elements of V that are not finite replaced by 0, and adds what is not finite to the rows that see it.
+#include <type_traits>
+
 #include "attn_packed_rows.h"
 
 namespace dare {
@@ -372,6 +374,309 @@ __global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedD
   }
 }
 
+// ---- many rows: 128 of them, four waves of 32 rows on the same keys --------------------------------
+// Tiles of 64 keys through two stages of K and two of V, shared by the waves.  A wave's keys are two stretches: the tiles that all of its
+// rows see whole, and the one to three behind them in which some row's keys end.
+// The first stretch runs as one stream of instructions over subtiles of 32 keys: while the logits of one are multiplied, the softmax of
+// the one before and the value product of the one before that run, an MFMA or two, an exponential, fragment reads, and so
+// on; fragments are read three MFMA groups ahead, and the barrier of a step lies behind its last fragment.  No mask in it,
+// and no maximum of every tile: the reference of a row moves when a lane's sum of probabilities says so.  (As attention over many rows
+// of one head does it, attn_bf16.hip, where this order was measured.)  The second stretch is plain: logits, mask, softmax, values.
+constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves, kManyKeys = 64;
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt_and_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(PackedDev p) {
+  constexpr int BM = kManyRows, CB = DH / 16, ROWB = DH * 2, TILE = kManyKeys * ROWB;
+  constexpr int CPR = DH / 8, RPL = 64 / CPR;      // 16-byte chunks per row, rows of a wave's load
+  constexpr int KL = TILE / 1024 / kManyWaves;     // a wave's loads of K (or V) per step
+  constexpr int NP = CB;                           // fragments of K, and of V, that a subtile takes
+  constexpr int AHEAD = 3, RING = AHEAD + 1;       // fragments read ahead of their MFMAs
+  static_assert(NP % RING == 0, "fragments must divide");
+  using Yes = std::true_type;
+  using No = std::false_type;
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, kq = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
+  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
+  Place at;
+  if (!find_block<BM>(p.rows, g, at)) return;
+
+  // steps of the block's part, and of them the wave's: those that all of its rows see whole, those that one of them sees
+  const int most = row_limit(p.rows, at, at.row0 + at.rows - 1);
+  const int tiles = (most + kManyKeys - 1) / kManyKeys, n_parts = parts_of(p, tiles);
+  if (part >= n_parts) return;
+  const int first = (int)((long)tiles * part / n_parts), n_steps = (int)((long)tiles * (part + 1) / n_parts) - first;
+  const bool any_row = wave * 32 < at.rows;  // (a wave without rows only loads)
+  int whole = 0, mine = 0;
+  if (any_row) {
+    const int last = wave * 32 + 31 < at.rows ? wave * 32 + 31 : at.rows - 1;
+    whole = row_limit(p.rows, at, at.row0 + wave * 32) / kManyKeys - first;
+    mine = (row_limit(p.rows, at, at.row0 + last) + kManyKeys - 1) / kManyKeys - first;
+    mine = mine < 0 ? 0 : mine < n_steps ? mine : n_steps;
+    whole = whole < 0 ? 0 : whole < mine ? whole : mine;
+  }
+  whole = __builtin_amdgcn_readfirstlane(whole);
+  mine = __builtin_amdgcn_readfirstlane(mine);
+
+  Rows<DH, 2> w;
+  long out_at[2];
+  take_rows(p, at, kvh, wave * 32, w, out_at);
+  w.clear();
+
+  // ---- global -> LDS ----
+  const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
+  const bf16_t* vbase = p.v + (long)at.k0 * p.ldv + kvh * DH;
+  const unsigned key0 = (unsigned)wave * KL * RPL + (unsigned)lane / CPR;  // key of this lane's first load of a step
+  // (the chunk XOR of a key is that of the lane's first key and that of the distance)
+  const unsigned k_chunk = ((unsigned)lane % CPR ^ k_swizzle<DH>(key0)) * 16, v_chunk = ((unsigned)lane % CPR ^ v_swizzle<DH>(key0)) * 16;
+  const unsigned lds0 = (unsigned)(size_t)(lptr_t)smem;
+  auto load_tiles = [&](auto is_v, int step) __attribute__((always_inline)) {
+    constexpr bool V = decltype(is_v)::value;
+    const int k0 = (first + step) * kManyKeys;
+    const unsigned row_bytes = (unsigned)(V ? p.ldv : p.ldk) * 2;
+    const bf16_t* from = V ? vbase + (long)k0 * p.ldv : kbase + (long)k0 * p.ldk;
+    const unsigned to = lds0 + (V ? 2 * TILE : 0) + (step & 1) * TILE + wave * KL * 1024;
+    const unsigned chunk = V ? v_chunk : k_chunk;
+    auto load = [&](unsigned a, const bf16_t* base, int i) __attribute__((always_inline)) {
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(a), "s"(base), "{m0}"(to + i * 1024) : "memory");
+    };
+#define DARE_SWZ(i) ((V ? v_swizzle<DH>((i) * RPL) : k_swizzle<DH>((i) * RPL)) * 16)
+    if (k0 + kManyKeys > at.len_k) {  // keys past the end re-read the last one
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        const unsigned key = key0 + i * RPL, end = at.len_k - 1 - k0;
+        load((key < end ? key : end) * row_bytes + (chunk ^ DARE_SWZ(i)), from, i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < KL; ++i) load((chunk ^ DARE_SWZ(i)) + key0 * row_bytes, from + (long)(i * RPL) * (V ? p.ldv : p.ldk), i);
+    }
+#undef DARE_SWZ
+  };
+  // Publishes K of step + 1 and V of step; every wave has read K of step and V of step - 1, whose stages are filled again
+  auto next_tiles = [&](int step) __attribute__((always_inline)) {
+    wait_vmcnt_and_barrier<0>();
+    if (step + 2 < n_steps) load_tiles(No{}, step + 2);
+    if (step + 1 < n_steps) load_tiles(Yes{}, step + 1);
+  };
+
+  // ---- fragments ----
+  // K fragment j: keys 16 (j & 1) + l16, channels 32 (j / 2) + 8 kq ..
+  // V fragment j, by transpose read: channel 16 j + l16, keys 4 kq .. +3 and 16 + 4 kq .. +3
+  unsigned k_at[NP / 2], v_at;
+#pragma unroll
+  for (int ks = 0; ks < NP / 2; ++ks) k_at[ks] = lds0 + l16 * ROWB + ((ks * 4 + kq) ^ k_swizzle<DH>(l16)) * 16;
+  {
+    const int key = kq * 4 + (l16 >> 2);
+    v_at = lds0 + 2 * TILE + key * ROWB + ((l16 >> 1 & 1) ^ v_swizzle<DH>(key)) * 16 + (l16 & 1) * 8;
+  }
+  bf16x8 kf[RING], vf[RING];
+  auto read_k = [&](int j, int sub) __attribute__((always_inline)) {
+    kf[j % RING] = *(lds_frag_t)(k_at[j / 2] + (sub * 32 + (j & 1) * 16) * ROWB);
+  };
+  auto read_v = [&](int j, int sub) __attribute__((always_inline)) {
+    const unsigned a = lds0 + ((v_at - lds0) ^ j * 32) + sub * 32 * ROWB;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(a + 16 * ROWB));
+    vf[j % RING] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  f32x4 sc[2][2][2];        // logits of two subtiles, [set][row block][16 keys]: keys 4 kq ..
+  bf16x8 pf[2][2];          // probabilities of two subtiles, [set][row block]
+
+  // ---- softmax of a subtile: logit n = 8 row block + key slot ----
+  const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+  float e0 = 0.f, e1 = 0.f;
+  auto exp_one = [&](const f32x4 (&x)[2][2], int n) __attribute__((always_inline)) {
+    const float v = __builtin_amdgcn_exp2f(fmaf(x[n >> 3][n >> 2 & 1][n & 3], p.scale_log2, -w.m[n >> 3]));
+    if (n & 1) e1 = v; else e0 = v;
+  };
+  auto round_pair = [&](bf16x8 (&pr)[2], int n, float (&sum)[2]) __attribute__((always_inline)) {
+    const f32x2 v = {e0, e1};
+    const bf16x2 pb = __builtin_convertvector(v, bf16x2);
+    sum[n >> 3] = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum[n >> 3], false);
+    pr[n >> 3][n & 7] = pb[0];
+    pr[n >> 3][(n & 7) + 1] = pb[1];
+  };
+  // The reference of the rows of a block of 16 moves to the maximum of this subtile, which is scored again, and of the next one, where
+  // that is 2^8 above it.  A probability below 256 is looked at by nobody: any reference gives the same result up to rounding.
+  // FIRST: there is none yet.
+  auto move_reference = [&](auto r_c, const f32x4 (&x)[2][2], const f32x4 (&next)[2][2], bf16x8 (&pr)[2], float (&sum)[2], auto first_c) __attribute__((always_inline)) {
+    constexpr int r = decltype(r_c)::value;
+    float top = x[r][0][0];
+#pragma unroll
+    for (int n = 1; n < 8; ++n) top = fmaxf(top, x[r][n >> 2][n & 3]);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) top = fmaxf(top, next[r][n >> 2][n & 3]);
+    top = row_max(top) * p.scale_log2;  // scale > 0
+    const float moved = top > w.m[r] + 8.f ? top : w.m[r];
+    const float m_new = fmaxf(moved, -__FLT_MAX__);  // (finite: logits of -infinity have probability 0)
+    if constexpr (!decltype(first_c)::value) {
+      const float alpha = __builtin_amdgcn_exp2f(w.m[r] - m_new);
+      w.l[r] *= alpha;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) w.acc[c][r] *= alpha;
+    }
+    w.m[r] = m_new;
+    sum[r] = 0.f;
+#pragma unroll
+    for (int n = 8 * r; n < 8 * r + 8; n += 2) {
+      exp_one(x, n);
+      exp_one(x, n + 1);
+      round_pair(pr, n, sum);
+    }
+  };
+
+  // One subtile period.  QK: logits of subtile u (into sc[S ^ 1]); SM: softmax of u - 1 (sc[S], into pf[S]); PV: values of
+  // u - 2 (pf[S ^ 1]).  MORE: a period follows.
+  auto period = [&](auto s_c, auto qk_c, auto sm_c, auto pv_c, auto more_c, int step) __attribute__((always_inline)) {
+    constexpr int S = decltype(s_c)::value, SUB = S ^ 1;  // SUB: subtile of its tile, of K and V alike
+    constexpr bool QK = decltype(qk_c)::value, SM = decltype(sm_c)::value, PV = decltype(pv_c)::value;
+    constexpr bool MORE = decltype(more_c)::value, EDGE = SUB == 1;  // EDGE: the step's tiles end here
+    constexpr int LPP = 16 / NP;        // logits per fragment
+    constexpr int SPLIT = NP - AHEAD;   // fragment behind whose MFMAs the step's last ones are in registers
+    float sum[2] = {0.f, 0.f};
+    auto softmax = [&](int from, int to) __attribute__((always_inline)) {
+      if constexpr (SM) {
+#pragma unroll
+        for (int n = from; n < to; ++n) {
+          if (n % 2 == 0 && n > 0) round_pair(pf[S], n - 2, sum);
+          exp_one(sc[S], n);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      f32x4 (&x)[2][2] = sc[S ^ 1];
+      if constexpr (QK) x[0][j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[j % RING], w.qf[0][j / 2], j < 2 ? zero : x[0][j & 1], 0, 0, 0);
+      softmax(j * LPP, j * LPP + LPP / 2);
+      if constexpr (QK) x[1][j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[j % RING], w.qf[1][j / 2], j < 2 ? zero : x[1][j & 1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (PV) w.acc[j][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j % RING], pf[S ^ 1][0], w.acc[j][0], 0, 0, 0);
+      softmax(j * LPP + LPP / 2, (j + 1) * LPP);
+      if constexpr (PV) w.acc[j][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j % RING], pf[S ^ 1][1], w.acc[j][1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j + AHEAD < NP) {
+        if constexpr (QK) read_k(j + AHEAD, SUB);
+        if constexpr (PV) read_v(j + AHEAD, SUB);
+      } else if constexpr (MORE && !EDGE) {
+        if constexpr (QK) read_k(j + AHEAD - NP, 1);
+        if constexpr (PV) read_v(j + AHEAD - NP, 1);
+      }
+      if constexpr (EDGE && MORE) {
+        if (j == SPLIT) {  // all of the step's fragments are in registers: its stages may be filled again
+          if constexpr (SM) asm volatile("" : "+v"(sum[0]), "+v"(sum[1]), "+v"(e0), "+v"(e1));  // (what is done so far stays in front of the branches)
+          next_tiles(step);
+#pragma unroll
+          for (int i = 0; i < NP / 2; ++i) k_at[i] = lds0 + ((k_at[i] - lds0) ^ TILE);
+          if constexpr (PV) v_at = lds0 + ((v_at - lds0) ^ TILE);
+        }
+        if (j > SPLIT) {
+          const int from = AHEAD * (j - SPLIT - 1) / (AHEAD - 1), to = AHEAD * (j - SPLIT) / (AHEAD - 1);
+#pragma unroll
+          for (int i = from; i < to; ++i) {
+            read_k(i, 0);
+            read_v(i, 0);
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (SM) {
+      round_pair(pf[S], 14, sum);
+      constexpr float kLimit = 256.f;
+      if (__any(fmaxf(sum[0], sum[1]) > kLimit)) {
+        if (__any(sum[0] > kLimit)) move_reference(S0{}, sc[S], sc[S ^ 1], pf[S], sum, No{});
+        if (__any(sum[1] > kLimit)) move_reference(S1{}, sc[S], sc[S ^ 1], pf[S], sum, No{});
+      }
+      w.l[0] += sum[0];
+      w.l[1] += sum[1];
+    }
+  };
+
+  if (n_steps > 0) {
+    load_tiles(No{}, 0);
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (waits for the queries and these keys)
+    wait_vmcnt_and_barrier<0>();
+    load_tiles(Yes{}, 0);
+    if (n_steps > 1) load_tiles(No{}, 1);
+  }
+  if (whole > 0) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) read_k(j, 0);
+    period(S1{}, Yes{}, No{}, No{}, Yes{}, 0);
+    period(S0{}, Yes{}, No{}, No{}, Yes{}, 0);
+    move_reference(S0{}, sc[0], sc[1], pf[0], w.l, Yes{});
+    move_reference(S1{}, sc[0], sc[1], pf[0], w.l, Yes{});
+    for (int step = 1; step < whole; ++step) {
+      period(S1{}, Yes{}, Yes{}, Yes{}, Yes{}, step);
+      period(S0{}, Yes{}, Yes{}, Yes{}, Yes{}, step);
+    }
+    period(S1{}, No{}, Yes{}, Yes{}, Yes{}, whole);
+    period(S0{}, No{}, No{}, Yes{}, No{}, whole);
+  }
+  // (all waves load, and join the barrier of every step)
+  for (int step = whole; step < n_steps; ++step) {
+    const unsigned kt = lds0 + (step & 1) * TILE, vt = kt + 2 * TILE;
+    const int key = (first + step) * kManyKeys;
+    f32x4 x[2][2][2];
+    if (step < mine) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) w.logits(kt + u * 32 * ROWB, x[u]);
+    }
+    next_tiles(step);
+    if (step < mine) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 pr[2];
+        w.mask(x[u], key + u * 32);
+        w.softmax(x[u], pr, p.scale_log2);
+        w.template values<true>(vt + u * 32 * ROWB, pr, key + u * 32, at.len_k);
+      }
+    }
+  }
+
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int row = wave * 32 + r * 16 + l16;
+    const float l = row_sum(w.l[r]);
+    if (row >= at.rows) continue;
+    if (n_parts > 1) {
+      float* slot = part_slot<DH, BM>(p, g, kvh, part);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(slot + row * DH + c * 16 + kq * 4) = w.acc[c][r];
+      if (kq == 0) {
+        slot[BM * DH + row] = w.m[r];
+        slot[BM * DH + BM + row] = l;
+      }
+      continue;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16_t* to = p.out + out_at[r] + kq * 4;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(w.acc[c][r][e] * inv);
+      *reinterpret_cast<bf16x4*>(to + c * 16) = o;
+    }
+  }
+}
+
 // ---- parts of a row's keys, joined in their order: a wave per row --------------------------------
 template <int DH, int BM, int KEYS>
 __global__ void __launch_bounds__(256) attn_packed_join_kernel(PackedDev p) {
@@ -422,9 +727,20 @@ hipError_t launch_few(PackedDev p, const PackedPlan& plan, hipStream_t s) {
 }
 
 template <int DH>
+hipError_t launch_many(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
+  hipLaunchKernelGGL(attn_packed_many_kernel<DH>, grid, dim3(kManyWaves * 64), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.parts == 1) return e;
+  hipLaunchKernelGGL((attn_packed_join_kernel<DH, kManyRows, kManyKeys>), dim3((unsigned)(plan.blocks * p.n_kv)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+template <int DH>
 hipError_t launch_dh(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
   if (plan.rows == 16) return launch_few<DH, 1>(p, plan, s);
-  return launch_few<DH, 2>(p, plan, s);
+  if (plan.rows == 32) return launch_few<DH, 2>(p, plan, s);
+  return launch_many<DH>(p, plan, s);
 }
 
 PackedPlan plan_of(const PackedArgs& a) {
@@ -453,7 +769,7 @@ hipError_t launch_attn_packed_bf16(const PackedArgs& a, hipStream_t s) {
   p.rows = packed_rows(a, plan.blocks);
   p.n_kv = a.n_kv_heads;
   p.max_parts = plan.parts;
-  p.part_tiles = plan.part_keys / kFewKeys;
+  p.part_tiles = plan.part_keys / (plan.rows == kManyRows ? kManyKeys : kFewKeys);
   p.parts = a.workspace;
   p.scale_log2 = a.scale * kLog2e;
   return a.head_dim == 128 ? launch_dh<128>(p, plan, s) : launch_dh<64>(p, plan, s);

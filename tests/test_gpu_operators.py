@@ -245,16 +245,15 @@ def test_attention(lengths, block, dtype, h, kv, d):
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 @pytest.mark.parametrize("lens", [[1, 2, 127, 128, 129], [511, 64, 700], [256, 1, 320, 33]])
-@pytest.mark.parametrize("block", [0, 1, 32])
-def test_attention_of_prompts(dtype, d, lens, block):
-    """Longer prompts, queries, keys and values parts of one buffer."""
+@pytest.mark.parametrize("block,h,kv,pad", [(0, 4, 2, 0), (1, 4, 2, 24), (32, 4, 2, 0), (1, 7, 1, 8), (1, 2, 2, 40)])
+def test_attention_of_prompts(dtype, d, lens, block, h, kv, pad):
+    """Longer prompts, queries, keys and values parts of one buffer, whose rows may end in something else."""
     g = _gen(sum(lens) + d)
-    h, kv = 4, 2
     off = _offsets(lens)
     qkv = ou.rand(g, off[-1], h + 2 * kv, d, dtype=dtype)
     q, k, v = qkv[:, :h], qkv[:, h:h + kv], qkv[:, h + kv:]
     want, bound, _ = ou.attention64(q, k, v, off, off[:-1], off[1:], block, d ** -0.5)
-    dev = qkv.cuda()
+    dev = _padded(qkv, pad)
     out = _run_attention(dev[:, :h], dev[:, h:h + kv], dev[:, h + kv:], off, off[:-1], off[1:], block)
     assert ou.worst(out, want, bound) <= 1.0
 
