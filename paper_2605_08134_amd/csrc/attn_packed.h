@@ -33,10 +33,17 @@ constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, i
   plan.blocks = (int)((long)total_q * group / plan.rows) + batch;
   plan.parts = 1;
   plan.part_keys = 1 << 30;
-  // As many parts as fill the 256 CUs about three times, of 256 keys at least
-  const long pairs = (long)plan.blocks * n_kv;
-  long parts = (plan.rows == 128 ? 512 : 768) / (pairs > 0 ? pairs : 1);
-  if (parts > max_k / 256) parts = max_k / 256;
+  // Few rows: parts of 512 keys, the unit that keeps a CU busy for longer than a workgroup takes to start and to end (384
+  // and 768: one token over each of 64 sequences of 500 to 8000 keys, 32 and 8 heads, 169 and 161 us for 159, over 32 of 40 to 4000 38 and
+  // 37 for 35); shorter ones, down to 128, where those do not give every CU two workgroups (8 sequences of 1000 keys: parts of 1000, 500
+  // and 128 XXX us); longer ones where there would be more than 64, or more than 16 rounds of workgroups, which even out
+  // by themselves.  Many rows: as many parts as give every CU two workgroups, of 512 keys at least.
+  // (blocks that hold rows, about: at least what the rows fill, at least one of every sequence)
+  const long filled = (long)total_q * group / plan.rows, some = batch < total_q ? batch : total_q;
+  const long pairs = (filled > some ? filled : some > 0 ? some : 1) * n_kv, room = (plan.rows == 128 ? 512 : 8192) / pairs;
+  const long even = max_k * pairs / 512;
+  long parts = max_k / (plan.rows == 128 || even > 512 ? 512 : even > 128 ? even : 128);
+  if (parts > room) parts = room;
   if (parts > kPackedMaxParts) parts = kPackedMaxParts;
   if (parts > 1) {
     plan.parts = (int)parts;

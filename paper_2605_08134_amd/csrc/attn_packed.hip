@@ -255,15 +255,18 @@ __device__ __forceinline__ float* part_slot(const PackedDev& p, int g, int kvh, 
   return p.parts + ((long)(g * p.n_kv + kvh) * p.max_parts + part) * packed_slot_floats(DH, BM);
 }
 
-// ---- few rows: 16 R of them, four waves that share the keys -------------------------------------
-// Every wave takes every fourth tile of 32 keys through two stages of its own, so that the waves meet at the end only.
-constexpr int kFewWaves = 4, kFewKeys = 32;
+// ---- few rows: 16 R of them, the keys shared by the waves -----------------------------------------
+// Every wave takes every second (heads of 64 channels: fourth) tile of 32 keys through two stages of its own, so that the waves meet at
+// the end only.  64 KB of stages per workgroup, two workgroups on a CU: one reads while the other starts or ends.
+constexpr int kFewKeys = 32;
+template <int DH>
+constexpr int kFewWaves = DH == 128 ? 2 : 4;
 
 template <int DH, int R>
-__global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedDev p) {
-  constexpr int BM = 16 * R, CB = DH / 16, TILE = kFewKeys * DH * 2, STAGE = 2 * TILE, L = TILE / 1024;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[kFewWaves * 2 * STAGE];
-  __shared__ float m_all[kFewWaves][R][16], l_all[kFewWaves][R][16];
+__global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(PackedDev p) {
+  constexpr int BM = 16 * R, CB = DH / 16, TILE = kFewKeys * DH * 2, STAGE = 2 * TILE, L = TILE / 1024, NW = kFewWaves<DH>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 2 * STAGE];
+  __shared__ float m_all[NW][R][16], l_all[NW][R][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kq = lane >> 4;
   const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
@@ -276,31 +279,30 @@ __global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedD
   if (part >= n_parts) return;
   const int first = (int)((long)tiles * part / n_parts), last = (int)((long)tiles * (part + 1) / n_parts);
 
-  Rows<DH, R> w;
-  long out_at[R];
-  take_rows(p, at, kvh, 0, w, out_at);
-  w.clear();
   const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
   const bf16_t* vbase = p.v + (long)at.k0 * p.ldv + kvh * DH;
   const unsigned lds0 = (unsigned)(size_t)(lptr_t)smem + wave * 2 * STAGE;
   auto load_k = [&](int t, int s) __attribute__((always_inline)) { load_rows<DH, kFewKeys, false>(kbase, p.ldk, t * kFewKeys, at.len_k, lds0 + s * STAGE); };
   auto load_v = [&](int t, int s) __attribute__((always_inline)) { load_rows<DH, kFewKeys, true>(vbase, p.ldv, t * kFewKeys, at.len_k, lds0 + s * STAGE + TILE); };
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (the queries are there)
-  wait_vmcnt<0>();
   int t = first + wave, s = 0;
   if (t < last) {
     load_k(t, 0);
     load_v(t, 0);
   }
-  if (t + kFewWaves < last) {
-    load_k(t + kFewWaves, 1);
-    load_v(t + kFewWaves, 1);
+  if (t + NW < last) {
+    load_k(t + NW, 1);
+    load_v(t + NW, 1);
   }
-  for (; t < last; t += kFewWaves, s ^= 1) {
-    const bool one = t + kFewWaves < last, two = t + 2 * kFewWaves < last;
+  Rows<DH, R> w;
+  long out_at[R];
+  take_rows(p, at, kvh, 0, w, out_at);
+  w.clear();
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (the queries in registers, or the loop waits for them in every step)
+  for (; t < last; t += NW, s ^= 1) {
+    const bool one = t + NW < last, two = t + 2 * NW < last;
     const unsigned kt = lds0 + s * STAGE, vt = kt + TILE;
     const int key0 = t * kFewKeys;
     const bool masked = key0 + kFewKeys > least;
@@ -309,13 +311,13 @@ __global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedD
     if (one) wait_vmcnt<3 * L>(); else wait_vmcnt<L>();
     w.logits(kt, x);
     wait_lds();
-    if (two) load_k(t + 2 * kFewWaves, s);
+    if (two) load_k(t + 2 * NW, s);
     if (masked) w.mask(x, key0);
     w.softmax(x, pf, p.scale_log2);
     if (two) wait_vmcnt<3 * L>(); else if (one) wait_vmcnt<2 * L>(); else wait_vmcnt<0>();
     if (masked) w.template values<true>(vt, pf, key0, at.len_k); else w.template values<false>(vt, pf, key0, at.len_k);
     wait_lds();
-    if (two) load_v(t + 2 * kFewWaves, s);
+    if (two) load_v(t + 2 * NW, s);
   }
 
   // ---- the waves' results are joined in their order, a share of the channel blocks by each ----
@@ -331,14 +333,14 @@ __global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedD
     for (int c = 0; c < CB; ++c) reinterpret_cast<f32x4*>(mine)[(c * R + r) * 64 + lane] = w.acc[c][r];
   }
   __syncthreads();
-  constexpr int OWN = CB / kFewWaves;
+  constexpr int OWN = CB / NW;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    float m = m_all[0][r][l16], l = 0.f, f[kFewWaves];
+    float m = m_all[0][r][l16], l = 0.f, f[NW];
 #pragma unroll
-    for (int o = 1; o < kFewWaves; ++o) m = fmaxf(m, m_all[o][r][l16]);
+    for (int o = 1; o < NW; ++o) m = fmaxf(m, m_all[o][r][l16]);
 #pragma unroll
-    for (int o = 0; o < kFewWaves; ++o) {
+    for (int o = 0; o < NW; ++o) {
       f[o] = __builtin_amdgcn_exp2f(m_all[o][r][l16] - m);
       l += l_all[o][r][l16] * f[o];
     }
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(kFewWaves * 64) attn_packed_few_kernel(PackedD
       const int c = wave * OWN + i;
       sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int o = 0; o < kFewWaves; ++o)
+      for (int o = 0; o < NW; ++o)
         sum[i] += reinterpret_cast<const f32x4*>(smem + o * 2 * STAGE)[(c * R + r) * 64 + lane] * f[o];
     }
     if (n_parts > 1) {
@@ -427,11 +429,6 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   whole = __builtin_amdgcn_readfirstlane(whole);
   mine = __builtin_amdgcn_readfirstlane(mine);
 
-  Rows<DH, 2> w;
-  long out_at[2];
-  take_rows(p, at, kvh, wave * 32, w, out_at);
-  w.clear();
-
   // ---- global -> LDS ----
   const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
   const bf16_t* vbase = p.v + (long)at.k0 * p.ldv + kvh * DH;
@@ -468,6 +465,17 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
     if (step + 2 < n_steps) load_tiles(No{}, step + 2);
     if (step + 1 < n_steps) load_tiles(Yes{}, step + 1);
   };
+
+  // The first tiles and the queries, all on their way at once: what a short sequence takes is latencies
+  if (n_steps > 0) {
+    load_tiles(No{}, 0);
+    load_tiles(Yes{}, 0);
+  }
+  if (n_steps > 1) load_tiles(No{}, 1);
+  Rows<DH, 2> w;
+  long out_at[2];
+  take_rows(p, at, kvh, wave * 32, w, out_at);
+  w.clear();
 
   // ---- fragments ----
   // K fragment j: keys 16 (j & 1) + l16, channels 32 (j / 2) + 8 kq ..
@@ -605,16 +613,11 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
     }
   };
 
-  if (n_steps > 0) {
-    load_tiles(No{}, 0);
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+  for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (waits for the queries and these keys)
-    wait_vmcnt_and_barrier<0>();
-    load_tiles(Yes{}, 0);
-    if (n_steps > 1) load_tiles(No{}, 1);
-  }
+    for (int ks = 0; ks < DH / 32; ++ks) asm volatile("" : "+v"(w.qf[r][ks]));  // (the queries in registers)
+  wait_vmcnt_and_barrier<0>();
   if (whole > 0) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) read_k(j, 0);
@@ -677,52 +680,119 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   }
 }
 
-// ---- parts of a row's keys, joined in their order: a wave per row --------------------------------
+// ---- parts of a row's keys, joined ---------------------------------------------------------------
+// What bounds both forms is the latency of what other XCDs have written; so all that a row needs is asked for at once.
+// The row (and its block) of a lane's token; false without one, or with one part
 template <int DH, int BM, int KEYS>
-__global__ void __launch_bounds__(256) attn_packed_join_kernel(PackedDev p) {
-  constexpr int PER = DH / 64;
-  typedef float vec_t __attribute__((ext_vector_type(PER)));
-  typedef __bf16 out_t __attribute__((ext_vector_type(PER)));
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ bool join_place(const PackedDev& p, int row, Place& at, const float*& slot, int& n_parts) {
   const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
-  Place at;
-  if (!find_block<BM>(p.rows, g, at)) return;
-  const int most = row_limit(p.rows, at, at.row0 + at.rows - 1);
-  const int n_parts = parts_of(p, (most + KEYS - 1) / KEYS);
-  if (n_parts < 2) return;
-  const float* slot = part_slot<DH, BM>(p, g, kvh, 0);
+  if (!find_block<BM>(p.rows, g, at) || row >= at.rows) return false;
+  n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + KEYS - 1) / KEYS);
+  slot = part_slot<DH, BM>(p, g, kvh, 0);
+  return n_parts > 1;
+}
+// channels c .. c + 3 of the row
+__device__ __forceinline__ void join_store(const PackedDev& p, const Place& at, int row, int c, int dh, f32x4 sum, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int j = at.row0 + row, i = (unsigned)j / (unsigned)p.rows.group;
+  const int head = (int)(blockIdx.x % p.n_kv) * p.rows.group + (j - i * p.rows.group);
+  bf16x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(sum[e] * inv);
+  *reinterpret_cast<bf16x4*>(p.out + (long)(at.q0 + i) * p.ldo + head * dh + c) = o;
+}
+
+// Few rows, up to 64 parts: a wave per row.  Lane q holds the reference and the sum of part q; DH / 4 lanes hold a part's channels, so
+// 2 (4) parts are read side by side, eight times that many at once.
+template <int DH, int BM>
+__global__ void __launch_bounds__(256) attn_packed_join_few_kernel(PackedDev p) {
+  constexpr int LANES = DH / 4, SIDE = 64 / LANES, AT_ONCE = 8;
   constexpr long SLOT = packed_slot_floats(DH, BM);
-  for (int row = wave; row < at.rows; row += 4) {
-    // (kMaxParts is at most the lanes of a wave)
-    const float m_own = lane < n_parts ? slot[lane * SLOT + BM * DH + row] : -__FLT_MAX__;
-    float m = m_own;
+  const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Place at;
+  const float* slot;
+  int n_parts;
+  if (!join_place<DH, BM, kFewKeys>(p, row, at, slot, n_parts)) return;
+  const int own = lane < n_parts ? lane : n_parts - 1, c = lane % LANES * 4, side = lane / LANES;
+  const float m_own = slot[own * SLOT + BM * DH + row], l_own = slot[own * SLOT + BM * DH + BM + row];
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float m, l, f_own;
+  for (int q0 = 0; q0 < n_parts; q0 += SIDE * AT_ONCE) {
+    f32x4 v[AT_ONCE];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    const float f_own = __builtin_amdgcn_exp2f(m_own - m);
-    const float l = wave_sum(lane < n_parts ? slot[lane * SLOT + BM * DH + BM + row] * f_own : 0.f);
-    vec_t sum;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) sum[e] = 0.f;
-    for (int q = 0; q < n_parts; ++q) {
-      const float f = __shfl(f_own, q, 64);
-      sum += *reinterpret_cast<const vec_t*>(slot + q * SLOT + row * DH + lane * PER) * f;
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int q = q0 + i * SIDE + side;
+      v[i] = *reinterpret_cast<const f32x4*>(slot + (q < n_parts ? q : n_parts - 1) * SLOT + row * DH + c);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int j = at.row0 + row, i = (unsigned)j / (unsigned)p.rows.group, head = kvh * p.rows.group + (j - i * p.rows.group);
-    out_t o;
+    __builtin_amdgcn_sched_barrier(0);
+    if (q0 == 0) {
+      m = m_own;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = (bf16_t)(sum[e] * inv);
-    *reinterpret_cast<out_t*>(p.out + (long)(at.q0 + i) * p.ldo + head * DH + lane * PER) = o;
+      for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+      f_own = lane < n_parts ? __builtin_amdgcn_exp2f(m_own - m) : 0.f;
+      l = wave_sum(l_own * f_own);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int q = q0 + i * SIDE + side;
+      const float f = __shfl(f_own, q & 63, 64);
+      if (q < n_parts) sum += v[i] * f;
+    }
   }
+#pragma unroll
+  for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o, 64);
+  if (side == 0) join_store(p, at, row, c, DH, sum, l);
+}
+
+// Many rows, few parts: a thread per row and four channels, four parts at once.
+template <int DH>
+__global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p) {
+  constexpr int LANES = DH / 4, AT_ONCE = 4, BM = kManyRows;
+  constexpr long SLOT = packed_slot_floats(DH, BM);
+  const int row = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+  Place at;
+  const float* slot;
+  int n_parts;
+  if (!join_place<DH, BM, kManyKeys>(p, row, at, slot, n_parts)) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float m = -__FLT_MAX__, l = 0.f;
+  for (int q0 = 0; q0 < n_parts; q0 += AT_ONCE) {
+    f32x4 v[AT_ONCE];
+    float mq[AT_ONCE], lq[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {  // (parts past the end: the last one again, for nothing)
+      const float* from = slot + (q0 + i < n_parts ? q0 + i : n_parts - 1) * SLOT;
+      mq[i] = from[BM * DH + row];
+      lq[i] = from[BM * DH + BM + row];
+      v[i] = *reinterpret_cast<const f32x4*>(from + row * DH + c);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    float m_new = m;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) m_new = fmaxf(m_new, mq[i]);
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    sum *= alpha;
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const float f = q0 + i < n_parts ? __builtin_amdgcn_exp2f(mq[i] - m) : 0.f;
+      if (q0 + i < n_parts) sum += v[i] * f;
+      l = fmaf(lq[i], f, l);
+    }
+  }
+  join_store(p, at, row, c, DH, sum, l);
 }
 
 template <int DH, int R>
 hipError_t launch_few(PackedDev p, const PackedPlan& plan, hipStream_t s) {
   const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
-  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R>), grid, dim3(kFewWaves * 64), 0, s, p);
-  hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R>), grid, dim3(kFewWaves<DH> * 64), 0, s, p);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.parts == 1) return e;
-  hipLaunchKernelGGL((attn_packed_join_kernel<DH, 16 * R, kFewKeys>), dim3((unsigned)(plan.blocks * p.n_kv)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((attn_packed_join_few_kernel<DH, 16 * R>), dim3((unsigned)(plan.blocks * p.n_kv), 4 * R), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -730,9 +800,9 @@ template <int DH>
 hipError_t launch_many(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
   const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
   hipLaunchKernelGGL(attn_packed_many_kernel<DH>, grid, dim3(kManyWaves * 64), 0, s, p);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.parts == 1) return e;
-  hipLaunchKernelGGL((attn_packed_join_kernel<DH, kManyRows, kManyKeys>), dim3((unsigned)(plan.blocks * p.n_kv)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(attn_packed_join_many_kernel<DH>, dim3((unsigned)(plan.blocks * p.n_kv), kManyRows * DH / 1024), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

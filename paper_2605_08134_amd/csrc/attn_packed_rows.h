@@ -36,24 +36,30 @@ __device__ __forceinline__ bool find_block(const PackedRows& p, const int g, Pla
     const int o = p.q_off[b];
     return o < 0 ? 0 : o > p.total_q ? p.total_q : o;
   };
+  auto number = [&](int off, int b) __attribute__((always_inline)) { return (int)((unsigned)(off * p.group) / BM) + b; };
   int lo = 0, n = p.batch;
-  while (n > 1) {  // 64 candidates at a time
+  while (n > 64) {  // 64 candidates at a time
     const int step = (n + 63) >> 6, b = lane * step;
-    const bool before = b < n && (int)((unsigned)(offset(lo + b) * p.group) / BM) + lo + b <= g;
-    const int count = __builtin_popcountll(__ballot(before));
+    const int count = __builtin_popcountll(__ballot(b < n && number(offset(lo + b), lo + b) <= g));
     if (count == 0) return false;
     lo += (count - 1) * step;
     n -= (count - 1) * step;
     n = n < step ? n : step;
   }
-  const int first = __builtin_amdgcn_readfirstlane(offset(lo)), end = __builtin_amdgcn_readfirstlane(offset(lo + 1));
+  // (the last round reads all that is to know of its candidates)
+  const int b = lo + (lane < n ? lane : n - 1);
+  const int own_first = offset(b), own_end = offset(b + 1), own_begin = p.k_begin[b], own_stop = p.k_end[b];
+  const int chosen = __builtin_popcountll(__ballot(lane < n && number(own_first, b) <= g)) - 1;
+  if (chosen < 0) return false;
+  lo += chosen;
+  const int first = __builtin_amdgcn_readlane(own_first, chosen), end = __builtin_amdgcn_readlane(own_end, chosen);
   const int len_q = end > first ? end - first : 0;
   at.q0 = first;
-  at.row0 = (g - lo - (int)((unsigned)(first * p.group) / BM)) * BM;
+  at.row0 = (g - number(first, lo)) * BM;
   const int rows = len_q * p.group - at.row0;
   if (at.row0 < 0 || rows <= 0) return false;
   at.rows = rows < BM ? rows : BM;
-  int begin = __builtin_amdgcn_readfirstlane(p.k_begin[lo]), stop = __builtin_amdgcn_readfirstlane(p.k_end[lo]);
+  int begin = __builtin_amdgcn_readlane(own_begin, chosen), stop = __builtin_amdgcn_readlane(own_stop, chosen);
   begin = begin < 0 ? 0 : begin > p.k_rows ? p.k_rows : begin;
   stop = stop > p.k_rows ? p.k_rows : stop;
   at.k0 = begin;
