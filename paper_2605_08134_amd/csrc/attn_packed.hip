@@ -45,6 +45,7 @@ struct PackedDev {
 
 typedef __attribute__((address_space(3))) void* lptr_t;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
 typedef const __attribute__((address_space(3))) bf16x8* lds_frag_t;
 typedef const __attribute__((address_space(3))) bf16_t* lds_elem_t;
@@ -184,28 +185,36 @@ struct Rows {
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
     const int key = kq * 4 + (l16 >> 2);
     const unsigned at = key * ROWB + ((l16 >> 1 & 1) ^ v_swizzle<DH>(key)) * 16 + (l16 & 1) * 8;
-    unsigned bad = 0;  // elements that are not finite: a bit of 0x80008000 each
+    u32x4 vf[CB];
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
       const unsigned va = vt + (at ^ (c * 32));
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(va));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(va + 16 * ROWB));
-      u32x4 w = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      if constexpr (MASKED) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned top = ((w[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponent of all ones
-          bad |= top;
-          w[i] &= ~((top >> 15) * 0xffffu);
-        }
-      }
-      const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-      for (int r = 0; r < R; ++r) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], acc[c][r], 0, 0, 0);
+      vf[c] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     if constexpr (MASKED) {
-      if (__builtin_expect(__any(bad != 0), 0)) add_not_finite(vt, key0, len_k);
+      u16x2 top = {0, 0};  // the largest elements without their signs
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[c][i] & 0x7fff7fffu));
+      if (__builtin_expect(__any(top[0] >= 0x7f80 || top[1] >= 0x7f80), 0)) {
+        add_not_finite(vt, key0, len_k);
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned ones = ((vf[c][i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // exponents of all ones
+            vf[c][i] &= ~((ones << 1) - (ones >> 15));
+          }
+      }
     }
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]), pf[r], acc[c][r], 0, 0, 0);
   }
 
   // What is not finite among the values, to the rows that see it (their probability is above 0)
@@ -404,6 +413,7 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];
+  __shared__ long out_rows[BM];  // where the rows' outputs lie
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kq = lane >> 4;
@@ -418,16 +428,18 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   if (part >= n_parts) return;
   const int first = (int)((long)tiles * part / n_parts), n_steps = (int)((long)tiles * (part + 1) / n_parts) - first;
   const bool any_row = wave * 32 < at.rows;  // (a wave without rows only loads)
-  int whole = 0, mine = 0;
+  int whole = 0, mine = 0, ends = 0;  // ends: keys that the wave's last row sees
   if (any_row) {
     const int last = wave * 32 + 31 < at.rows ? wave * 32 + 31 : at.rows - 1;
     whole = row_limit(p.rows, at, at.row0 + wave * 32) / kManyKeys - first;
-    mine = (row_limit(p.rows, at, at.row0 + last) + kManyKeys - 1) / kManyKeys - first;
+    ends = row_limit(p.rows, at, at.row0 + last);
+    mine = (ends + kManyKeys - 1) / kManyKeys - first;
     mine = mine < 0 ? 0 : mine < n_steps ? mine : n_steps;
     whole = whole < 0 ? 0 : whole < mine ? whole : mine;
   }
   whole = __builtin_amdgcn_readfirstlane(whole);
   mine = __builtin_amdgcn_readfirstlane(mine);
+  ends = __builtin_amdgcn_readfirstlane(ends);
 
   // ---- global -> LDS ----
   const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
@@ -476,6 +488,10 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   long out_at[2];
   take_rows(p, at, kvh, wave * 32, w, out_at);
   w.clear();
+  if (kq == 0) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) out_rows[wave * 32 + r * 16 + l16] = out_at[r];
+  }
 
   // ---- fragments ----
   // K fragment j: keys 16 (j & 1) + l16, channels 32 (j / 2) + 8 kq ..
@@ -639,12 +655,14 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
     f32x4 x[2][2][2];
     if (step < mine) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) w.logits(kt + u * 32 * ROWB, x[u]);
+      for (int u = 0; u < 2; ++u)
+        if (key + u * 32 < ends) w.logits(kt + u * 32 * ROWB, x[u]);
     }
     next_tiles(step);
     if (step < mine) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        if (key + u * 32 >= ends) break;
         bf16x8 pr[2];
         w.mask(x[u], key + u * 32);
         w.softmax(x[u], pr, p.scale_log2);
@@ -653,30 +671,46 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
     }
   }
 
+  float l[2];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int row = wave * 32 + r * 16 + l16;
-    const float l = row_sum(w.l[r]);
-    if (row >= at.rows) continue;
-    if (n_parts > 1) {
-      float* slot = part_slot<DH, BM>(p, g, kvh, part);
+  for (int r = 0; r < 2; ++r) l[r] = row_sum(w.l[r]);
+  if (n_parts > 1) {
+    float* slot = part_slot<DH, BM>(p, g, kvh, part);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = wave * 32 + r * 16 + l16;
+      if (row >= at.rows) continue;
 #pragma unroll
       for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(slot + row * DH + c * 16 + kq * 4) = w.acc[c][r];
       if (kq == 0) {
         slot[BM * DH + row] = w.m[r];
-        slot[BM * DH + BM + row] = l;
+        slot[BM * DH + BM + row] = l[r];
       }
-      continue;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    bf16_t* to = p.out + out_at[r] + kq * 4;
+    return;
+  }
+  // Outputs go through the wave's share of the K stages, which nobody reads behind the last barrier, so that a store has whole rows:
+  // as the sums lie, 32 bytes of 16 rows each, the stores of a workgroup took 3900 cycles.
+  const unsigned own = wave * 32 * ROWB;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
       bf16x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = (bf16_t)(w.acc[c][r][e] * inv);
-      *reinterpret_cast<bf16x4*>(to + c * 16) = o;
+      *reinterpret_cast<bf16x4*>(smem + own + (r * 16 + l16) * ROWB + ((c * 2 + (kq >> 1)) ^ (l16 % CPR)) * 16 + (kq & 1) * 8) = o;
     }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+  for (int i = 0; i < 32 / RPL; ++i) {
+    const int row = i * RPL + lane / CPR, chunk = lane % CPR;
+    const u32x4 o = *reinterpret_cast<const u32x4*>(smem + own + row * ROWB + (chunk ^ (row % CPR)) * 16);
+    if (wave * 32 + row < at.rows) *reinterpret_cast<u32x4*>(p.out + out_rows[wave * 32 + row] + chunk * 8) = o;
   }
 }
 
