@@ -4,14 +4,30 @@
 
 namespace dare {
 
+// j / d for 0 <= j < 2^31 by a product: with 2^(L - 1) < d <= 2^L and mul = ceil(2^(31 + L) / d), which is below 2^32, j mul / 2^(31 +
+// L) lies above j / d by less than j 2^L / (d 2^(31 + L)) < 1 / d.  (An exact division takes 40 instructions of a wave that has
+// nothing else to do yet.)
+struct Divider {
+  unsigned mul;
+  int shift;
+};
+constexpr Divider divider(unsigned d) {
+  int log = 0;
+  while ((1ull << log) < d) ++log;
+  return {(unsigned)(((1ull << (31 + log)) + d - 1) / d), 31 + log};
+}
+constexpr __attribute__((always_inline)) int divide(int j, Divider by) {
+  return (int)(((unsigned long long)(unsigned)j * by.mul) >> by.shift);
+}
+
 // Keys that token i of a sequence sees: a prefix of its len_k keys.  shift = len_k - len_q: the queries are the last
 // positions.  block 0: all; else up to the end of the token's block of that many positions.  A token in front of the
 // first key (negative position) sees none.
-constexpr __attribute__((always_inline)) int packed_limit(int i, int shift, int len_k, int block) {
+constexpr __attribute__((always_inline)) int packed_limit(int i, int shift, int len_k, int block, Divider by_block) {
   if (block == 0) return len_k;
   const int pos = i + shift;
   if (pos < 0) return 0;
-  const unsigned end = ((unsigned)pos / (unsigned)block + 1u) * (unsigned)block;  // (at most pos + block < 2^32)
+  const unsigned end = ((unsigned)divide(pos, by_block) + 1u) * (unsigned)block;  // (at most pos + block < 2^32)
   return end < (unsigned)len_k ? (int)end : len_k;
 }
 

@@ -89,16 +89,6 @@ __device__ __forceinline__ void load_rows(const bf16_t* base, long ld, int first
   }
 }
 
-// Maximum over the lanes L, L ^ 16, L ^ 32 and L ^ 48, which hold the same row
-__device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float row_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
-
 // 32 keys against R blocks of 16 rows.  kt, vt: LDS addresses of the keys' rows; key0: number of the first one.
 // MASKED: row r of a lane sees keys below lim[r] only.
 template <int DH, int R>
@@ -246,12 +236,12 @@ __device__ __forceinline__ void take_rows(const PackedDev& p, const Place& at, i
   for (int r = 0; r < R; ++r) {
     int j = row0 + r * 16 + l16;
     j = at.row0 + (j < at.rows ? j : at.rows - 1);
-    const int i = (unsigned)j / (unsigned)p.rows.group, head = kvh * p.rows.group + (j - i * p.rows.group);
+    const int i = divide(j, p.rows.by_group), head = kvh * p.rows.group + (j - i * p.rows.group);
     const bf16_t* row = p.q + (long)(at.q0 + i) * p.ldq + head * DH + kq * 8;
 #pragma unroll
     for (int ks = 0; ks < DH / 32; ++ks) w.qf[r][ks] = *reinterpret_cast<const bf16x8*>(row + ks * 32);
     out_at[r] = (long)(at.q0 + i) * p.ldo + head * DH;
-    w.lim[r] = packed_limit(i, at.shift, at.len_k, p.rows.causal_block);
+    w.lim[r] = packed_limit(i, at.shift, at.len_k, p.rows.causal_block, p.rows.by_causal_block);
   }
 }
 __device__ __forceinline__ int parts_of(const PackedDev& p, int tiles) {
@@ -728,7 +718,7 @@ __device__ __forceinline__ bool join_place(const PackedDev& p, int row, Place& a
 // channels c .. c + 3 of the row
 __device__ __forceinline__ void join_store(const PackedDev& p, const Place& at, int row, int c, int dh, f32x4 sum, float l) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int j = at.row0 + row, i = (unsigned)j / (unsigned)p.rows.group;
+  const int j = at.row0 + row, i = divide(j, p.rows.by_group);
   const int head = (int)(blockIdx.x % p.n_kv) * p.rows.group + (j - i * p.rows.group);
   bf16x4 o;
 #pragma unroll

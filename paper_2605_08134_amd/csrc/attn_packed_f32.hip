@@ -35,9 +35,9 @@ __global__ void __launch_bounds__(kWaves * 64) attn_packed_f32_kernel(PackedF32D
   const int least = row_limit(p.rows, at, at.row0), most = row_limit(p.rows, at, at.row0 + at.rows - 1);
 
   const bool valid = l16 < at.rows;
-  const int j = at.row0 + (valid ? l16 : at.rows - 1), i = (unsigned)j / (unsigned)p.rows.group;
+  const int j = at.row0 + (valid ? l16 : at.rows - 1), i = divide(j, p.rows.by_group);
   const int head = kvh * p.rows.group + (j - i * p.rows.group);
-  const int lim = packed_limit(i, at.shift, at.len_k, p.rows.causal_block);
+  const int lim = packed_limit(i, at.shift, at.len_k, p.rows.causal_block, p.rows.by_causal_block);
   const float* qrow = p.q + (long)(at.q0 + i) * p.ldq + head * DH + kq * 4;
   f32x4 qf[C], acc[C];
 #pragma unroll
@@ -76,8 +76,7 @@ __global__ void __launch_bounds__(kWaves * 64) attn_packed_f32_kernel(PackedF32D
       z[e] = key0 + kq * 4 + e < lim ? z[e] * p.scale : -INFINITY;
       top = fmaxf(top, z[e]);
     }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = row_max(top);
     const float m_new = fmaxf(m_run, top);  // (finite from below: a row that sees nothing has probabilities 0)
     const float alpha = expf(m_run - m_new);
     m_run = m_new;
@@ -113,8 +112,7 @@ __global__ void __launch_bounds__(kWaves * 64) attn_packed_f32_kernel(PackedF32D
         }
     }
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  l_run = row_sum(l_run);
   if (kq == 0) {
     m_part[wave][l16] = m_run;
     l_part[wave][l16] = l_run;

@@ -15,10 +15,12 @@ struct PackedRows {
   int group;         // query heads per key head
   int causal_block;
   int n_blocks;      // row blocks launched
+  Divider by_group, by_causal_block;
 };
 
 inline PackedRows packed_rows(const PackedArgs& a, int n_blocks) {
-  return {a.q_off, a.k_begin, a.k_end, a.batch, a.total_q, a.k_rows, a.n_heads / a.n_kv_heads, a.causal_block, n_blocks};
+  return {a.q_off, a.k_begin, a.k_end, a.batch, a.total_q, a.k_rows, a.n_heads / a.n_kv_heads, a.causal_block, n_blocks,
+          divider(a.n_heads / a.n_kv_heads), divider(a.causal_block ? a.causal_block : 1)};
 }
 
 struct Place {
@@ -70,7 +72,26 @@ __device__ __forceinline__ bool find_block(const PackedRows& p, const int g, Pla
 
 // Keys that row j of the sequence sees
 __device__ __forceinline__ int row_limit(const PackedRows& p, const Place& at, int j) {
-  return packed_limit((unsigned)j / (unsigned)p.group, at.shift, at.len_k, p.causal_block);
+  return packed_limit(divide(j, p.by_group), at.shift, at.len_k, p.causal_block, p.by_causal_block);
+}
+
+// All four lanes L, L ^ 16, L ^ 32 and L ^ 48, which hold the same row: maximum, sum.  (The swap's words are copied before they are taken
+// for floats: __builtin_bit_cast of an element of a vector reads the first one.)
+template <class Join>
+__device__ __forceinline__ float row_join(float x, Join join) {
+  const unsigned own = __builtin_bit_cast(unsigned, x);
+  const auto rows = __builtin_amdgcn_permlane16_swap(own, own, false, false);
+  const unsigned even = rows[0], odd = rows[1];
+  const unsigned pair = __builtin_bit_cast(unsigned, join(__builtin_bit_cast(float, even), __builtin_bit_cast(float, odd)));
+  const auto halves = __builtin_amdgcn_permlane32_swap(pair, pair, false, false);
+  const unsigned low = halves[0], high = halves[1];
+  return join(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+}
+__device__ __forceinline__ float row_max(float x) {
+  return row_join(x, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float row_sum(float x) {
+  return row_join(x, [](float a, float b) __attribute__((always_inline)) { return a + b; });
 }
 
 }  // namespace dare

@@ -146,8 +146,28 @@ int main(int n, char** a) {
     for (int lq = 1; lq < 12; ++lq)
       for (int lk = 0; lk < 14; ++lk)
         for (int block = 0; block < 9; ++block)
-          for (int i = 0; i < lq; ++i) std::printf("%d ", dare::packed_limit(i, lk - lq, lk, block));
-    std::printf("%d %d", dare::packed_limit(5, 0, 10, 2147483647), dare::packed_limit(2147483645, 0, 2147483647, 2147483647));
+          for (int i = 0; i < lq; ++i) std::printf("%d ", dare::packed_limit(i, lk - lq, lk, block, dare::divider(block ? block : 1)));
+    const dare::Divider most = dare::divider(2147483647);
+    std::printf("%d %d", dare::packed_limit(5, 0, 10, 2147483647, most), dare::packed_limit(2147483645, 0, 2147483647, 2147483647, most));
+    return 0;
+  }
+  if (n == 3) {  // divisions, at the ends of quotients and of the range
+    long wrong = 0;
+    unsigned seed = 1;
+    for (int k = 0; k < 3000; ++k) {
+      seed = seed * 1664525u + 1013904223u;
+      const unsigned d = k < 1000 ? k + 1 : k < 1031 ? 1u << (k - 1000) : (seed >> 1 >> (seed & 31) % 31) + 1;
+      if (d > 2147483647u) continue;
+      const dare::Divider by = dare::divider(d);
+      for (unsigned q = 0; q < 2000; ++q) {
+        seed = seed * 1664525u + 1013904223u;
+        const unsigned long long at = (unsigned long long)(q < 1000 ? q : seed % (2147483647u / d + 1)) * d;
+        for (long j = (long)at - 1; j <= (long)at + 1; ++j)
+          if (j >= 0 && j < 2147483648l) wrong += dare::divide((int)j, by) != (int)((unsigned)j / d);
+      }
+      wrong += dare::divide(2147483647, by) != (int)(2147483647u / d);
+    }
+    std::printf("%ld", wrong);
     return 0;
   }
   const dare::PackedPlan p = dare::packed_plan(atoi(a[1]), atoi(a[2]), atoi(a[3]), atoi(a[4]), atoi(a[5]), atoi(a[6]));
@@ -176,6 +196,10 @@ def test_keys_that_a_token_sees(probe):
     assert list(got) == [10, 2147483646 + 1]
 
 
+def test_division_by_a_product(probe):
+    assert probe("divide", "all") == [0]
+
+
 @pytest.mark.parametrize("batch", [1, 3, 32, 257])
 @pytest.mark.parametrize("max_q", [1, 4, 33, 5000])
 @pytest.mark.parametrize("max_k", [1, 300, 4096, 131072])
@@ -191,4 +215,4 @@ def test_the_plan_covers_every_row_and_key(probe, batch, max_q, max_k, group, kv
     assert start[batch] <= blocks
     assert 1 <= parts <= 64 and keys * parts >= max_k
     if parts > 1:
-        assert keys % 32 == 0 and keys >= 256 and -(-max_k // keys) <= parts
+        assert keys % 64 == 0 and keys >= 128 and -(-max_k // keys) <= parts
