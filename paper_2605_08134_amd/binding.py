@@ -541,82 +541,87 @@ def dare_k_copy_rows(src, dst, idx=None, m_dev=None, stream=None):
 
 
 # ---- decoder layers with shared key heads ------------------------------------------------
+# (A call takes the host about as long as a small kernel the GPU, so every property of a tensor is asked for once.)
 
-def _dtype_of(t):
+def _gpu_of(like):
+    """Device index and dtype code of the tensor that the others have to match."""
     import torch
-    if t.dtype == torch.bfloat16:
-        return DARE_BF16
-    if t.dtype == torch.float32:
-        return DARE_F32
-    raise ValueError("dtype must be bfloat16 or float32, not %s" % t.dtype)
-
-
-def _on_device(like, **tensors):
-    """Every tensor that is given lies on the GPU of `like`."""
-    if not like.is_cuda:
+    device, dt = like.get_device(), like.dtype
+    if device < 0:
         raise ValueError("tensors must be on the GPU")
-    for name, t in tensors.items():
-        if t is not None and t.device != like.device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, like.device))
+    if dt is torch.bfloat16:
+        return device, dt, DARE_BF16
+    if dt is torch.float32:
+        return device, dt, DARE_F32
+    raise ValueError("dtype must be bfloat16 or float32, not %s" % dt)
 
 
-def _heads(name, t, like, n=None, heads=None, head_dim=None):
-    """Pointer and row distance of a [tokens, heads, head_dim] tensor whose heads lie one behind the other."""
-    if t.dim() != 3 or t.dtype != like.dtype:
-        raise ValueError("%s must be [tokens, heads, head_dim] of the queries' dtype" % name)
-    rows, h, d = t.shape
-    if (n is not None and rows != n) or (heads is not None and h != heads) or (head_dim is not None and d != head_dim):
-        raise ValueError("%s has the shape %s" % (name, tuple(t.shape)))
-    if t.numel() and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
-        raise ValueError("the heads of a row of %s must lie one behind the other" % name)
-    return t.data_ptr(), t.stride(0) if rows > 1 else h * d
+def _wrong(name, t, dt, device, wanted):
+    raise ValueError("%s must be %s of %s on cuda:%d, is %s of %s on %s" % (name, wanted, dt, device, tuple(t.shape), t.dtype,
+                                                                       t.device))
 
 
-def _matrix(name, t, like, rows, cols):
+def _heads(name, t, dt, device, n, heads, head_dim):
+    """Pointer and row distance of a [n, heads, head_dim] tensor (None: any) whose heads lie one behind the other."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dt or t.get_device() != device:
+        _wrong(name, t, dt, device, "[tokens, heads, head_dim]")
+    rows, h, d = shape
+    if rows != n and n is not None or h != heads and heads is not None or d != head_dim:
+        _wrong(name, t, dt, device, "[%s, %s, %s]" % (n, heads, head_dim))
+    ld, between, inside = t.stride()
+    if inside != 1 and d > 1 or between != d and h > 1:
+        if t.numel():
+            raise ValueError("the heads of a row of %s must lie one behind the other" % name)
+    return t.data_ptr(), ld if rows > 1 else h * d
+
+
+def _matrix(name, t, dt, device, rows, cols):
     """Pointer and row distance of a [rows, cols] tensor with contiguous rows."""
-    if t.shape != (rows, cols) or t.dtype != like.dtype:
-        raise ValueError("%s must be [%d, %d] of dtype %s" % (name, rows, cols, like.dtype))
-    if t.numel() and cols > 1 and t.stride(1) != 1:
+    if t.shape != (rows, cols) or t.dtype is not dt or t.get_device() != device:
+        _wrong(name, t, dt, device, "[%s, %s]" % (rows, cols))
+    ld, inside = t.stride()
+    if inside != 1 and cols > 1 and rows:
         raise ValueError("the rows of %s must be contiguous" % name)
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
-def _ints(name, t, n):
-    import torch
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of %d elements" % (name, n))
+def _vector(name, t, dt, device, n):
+    if t.shape != (n,) or t.dtype is not dt or t.get_device() != device or not t.is_contiguous():
+        _wrong(name, t, dt, device, "a contiguous [%s]" % n)
     return t.data_ptr()
 
 
-def _enqueue(like, stream, fn, *args):
-    """fn(*args, stream) with the device of `like` as the current one."""
+def _enqueue(device, stream, fn, *args):
+    """fn(*args, stream) with `device` as the current one."""
     import torch
-    if stream is not None and stream.device != like.device:
-        raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, like.device))
-    if like.device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)))
+    if stream is not None and stream.device.index != device:
+        raise ValueError("the stream belongs to %s, the tensors to cuda:%d" % (stream.device, device))
+    if device == torch._C._cuda_getDevice():
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(like.device):
-            _check(fn(*args, _stream(stream)))
+        with torch.cuda.device(device):
+            st = fn(*args, _stream(stream))
+    if st:
+        _check(st)
 
 
 def dare_k_linear(a, wt, out, bias=None, act=None, residual=None, stream=None):
     """out = act(a W + bias) + residual.  a [m, k], out and residual [m, n] with contiguous rows, wt [n, k] packed
     (dare_k_pack_weight), act None, "silu", "gelu" or "gelu_tanh"; out may be residual."""
-    _on_device(a, wt=wt, out=out, bias=bias, residual=residual)
+    device, dt, code = _gpu_of(a)
+    if wt.dim() != 2 or a.dim() != 2 or act not in ACTIVATIONS:
+        raise ValueError("a and wt must be matrices, act one of %s" % list(ACTIVATIONS))
     n, k = wt.shape
     m = a.shape[0]
-    pa, lda = _matrix("a", a, a, m, k)
-    po, ldo = _matrix("out", out, a, m, n)
-    pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, a, m, n)
-    if wt.dtype != a.dtype or not wt.is_contiguous():
-        raise ValueError("wt must be contiguous, of the dtype of a")
-    if bias is not None and (bias.shape != (n,) or bias.dtype != a.dtype or not bias.is_contiguous()):
-        raise ValueError("bias must be [%d] of the dtype of a" % n)
-    if act not in ACTIVATIONS:
-        raise ValueError("act must be one of %s" % list(ACTIVATIONS))
-    _enqueue(a, stream, lib().dare_k_linear, _dtype_of(a), pa, lda, wt.data_ptr(), n, k, m,
-             None if bias is None else bias.data_ptr(), ACTIVATIONS[act], pr, ldr, po, ldo)
+    pa, lda = _matrix("a", a, dt, device, m, k)
+    po, ldo = _matrix("out", out, dt, device, m, n)
+    pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, dt, device, m, n)
+    pw, ldw = _matrix("wt", wt, dt, device, n, k)
+    if ldw != k:
+        raise ValueError("wt must be contiguous")
+    pb = None if bias is None else _vector("bias", bias, dt, device, n)
+    _enqueue(device, stream, lib().dare_k_linear, code, pa, lda, pw, n, k, m, pb, ACTIVATIONS[act], pr, ldr, po, ldo)
 
 
 def dare_k_rope_freqs(rot_dim, base=10000.0, scaling=None, factor=1.0, context=8192, low=1.0, high=4.0, device="cuda"):
@@ -638,36 +643,29 @@ def dare_k_rope(pos, freqs, layout="half", q=None, q_out=None, k=None, k_out=Non
     to.  layout "half" or "pairs"."""
     import torch
     first = q if q is not None else k if k is not None else v
-    if first is None:
-        raise ValueError("nothing to rotate")
-    if layout not in ROPE_LAYOUTS:
-        raise ValueError("layout must be one of %s" % list(ROPE_LAYOUTS))
-    _on_device(first, pos=pos, freqs=freqs, q=q, q_out=q_out, k=k, k_out=k_out, v=v, v_out=v_out, rows=rows)
-    n, d = first.shape[0], first.shape[2] if first.dim() == 3 else 0
-    kv = k if k is not None else v
-    args, out_rows = [], 0
-    for name, x, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
-        if (x is None) != (out is None):
-            raise ValueError("%s and %s_out go together" % (name, name))
+    if first is None or first.dim() != 3 or layout not in ROPE_LAYOUTS:
+        raise ValueError("q, k or v must be [tokens, heads, head_dim], layout one of %s" % list(ROPE_LAYOUTS))
+    device, dt, code = _gpu_of(first)
+    n, h, d = first.shape
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
+        raise ValueError("an input and its output go together")
+    if q is None:
+        args = [None, 0, None, 0, 0]
+    else:
+        args = [*_heads("q", q, dt, device, n, h, d), *_heads("q_out", q_out, dt, device, n, h, d), h]
+    kv, out_rows, n_out = None, 0, n if rows is None else None
+    for name, x, out in (("k", k, k_out), ("v", v, v_out)):
         if x is None:
             args += [None, 0, None, 0]
             continue
-        heads = None if name == "q" else kv.shape[1] if kv.dim() == 3 else -1
-        args += _heads(name, x, first, n, heads, d)
-        scattered = rows is not None and name != "q"
-        args += _heads(name + "_out", out, first, None if scattered else n, x.shape[1], d)
-        if scattered:
-            if out_rows and out.shape[0] != out_rows:
-                raise ValueError("k_out and v_out must have as many rows as each other")
-            out_rows = out.shape[0]
-    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
-        raise ValueError("freqs must be a contiguous float64 vector")
-    pr = None if rows is None else _ints("rows", rows, n)
-    if rows is not None and (kv is None or out_rows == 0):
-        raise ValueError("rows without k or v, or without rows to write")
-    _enqueue(first, stream, lib().dare_k_rope, _dtype_of(first), ROPE_LAYOUTS[layout], n, d, 2 * freqs.shape[0],
-             _ints("pos", pos, n), freqs.data_ptr(), magnitude, *args[:4], 0 if q is None else q.shape[1], *args[4:],
-             0 if kv is None else kv.shape[1], pr, out_rows)
+        args += _heads(name, x, dt, device, n, kv, d)
+        kv = x.shape[1]
+        args += _heads(name + "_out", out, dt, device, n_out, kv, d)
+        n_out = out_rows = out.shape[0]
+    half = freqs.shape[0]
+    _enqueue(device, stream, lib().dare_k_rope, code, ROPE_LAYOUTS[layout], n, d, 2 * half,
+             _vector("pos", pos, torch.int32, device, n), _vector("freqs", freqs, torch.float64, device, half), magnitude, *args,
+             kv or 0, None if rows is None else _vector("rows", rows, torch.int32, device, n), out_rows)
 
 
 def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, causal_block=0, scale=None,
@@ -677,24 +675,31 @@ def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, c
     sequence, b: those up to the end of its block of b positions (1: causal).  scale: 1 / sqrt(head_dim).  max_q, max_k: the largest
     numbers of query tokens and keys of a sequence.  workspace: a uint8 tensor of dare_k_attention_packed_workspace() bytes to
     use instead of one of the call's own."""
-    _on_device(q, k=k, v=v, out=out, q_off=q_off, k_begin=k_begin, k_end=k_end, workspace=workspace)
-    pq, ldq = _heads("q", q, q)
+    import torch
+    device, dt, code = _gpu_of(q)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
     total, h, d = q.shape
-    pk, ldk = _heads("k", k, q, None, None, d)
     rows, kv, _ = k.shape
-    pv, ldv = _heads("v", v, q, rows, kv, d)
-    po, ldo = _heads("out", out, q, total, h, d)
     batch = k_begin.shape[0]
-    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), _dtype_of(q), batch, total, rows, max_q, max_k, h, kv, d,
-                           causal_block, d ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
-    ref = ctypes.byref(cfg)
-    offsets = _ints("q_off", q_off, batch + 1), _ints("k_begin", k_begin, batch), _ints("k_end", k_end, batch)
-    need = ctypes.c_size_t()
-    _check(lib().dare_k_attention_packed_workspace(ref, ctypes.byref(need)))
-    if workspace is None and need.value:
-        workspace = _scratch(need.value, q.device, stream)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _enqueue(q, stream, lib().dare_k_attention_packed, ref, pq, pk, pv, po, *offsets, _ptr(workspace), size)
+    pq, ldq = _heads("q", q, dt, device, total, h, d)
+    pk, ldk = _heads("k", k, dt, device, rows, kv, d)
+    pv, ldv = _heads("v", v, dt, device, rows, kv, d)
+    po, ldo = _heads("out", out, dt, device, total, h, d)
+    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), code, batch, total, rows, max_q, max_k, h, kv, d, causal_block,
+                           d ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
+    ref, i32 = ctypes.byref(cfg), torch.int32
+    offsets = (_vector("q_off", q_off, i32, device, batch + 1), _vector("k_begin", k_begin, i32, device, batch),
+               _vector("k_end", k_end, i32, device, batch))
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().dare_k_attention_packed_workspace(ref, ctypes.byref(need)))
+        if need.value:
+            workspace = _scratch(need.value, q.device, stream)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on cuda:%d" % device)
+    pw, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _enqueue(device, stream, lib().dare_k_attention_packed, ref, pq, pk, pv, po, *offsets, pw, size)
 
 
 def dare_k_attention_packed_workspace(dtype, batch, total_q, max_q, max_k, n_heads, n_kv_heads, head_dim):
