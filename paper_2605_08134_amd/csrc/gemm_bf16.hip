@@ -152,7 +152,7 @@ __device__ __forceinline__ float silu(float g) {
 // Activation of N values at once: what it is is settled outside the loop.  Reciprocals and exponentials by the hardware's
 // instructions, 1 ulp of fp32 each, behind them a rounding to bf16.
 // GELU: z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt(2)) / 2 with erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2), t = 1 / (1 + p x)
-// (Abramowitz and Stegun, 7.1.26), 1.5e-7 off at most: a sixth of the instructions of a full erfc.
+// (Abramowitz and Stegun, 7.1.26), 1.5e-7 off at most, in 14 instructions.
 // Tanh form: z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
 template <int N>
 __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
@@ -162,12 +162,13 @@ __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
   } else if (act == DARE_ACT_GELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float z = v[i], x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-      float e = fmaf(t, 1.061405429f, -1.453152027f);
-      e = fmaf(t, e, 1.421413741f);
-      e = fmaf(t, e, -0.284496736f);
-      e = fmaf(t, e, 0.254829592f) * t * __builtin_amdgcn_exp2f(-0.72134752f * z * z);
-      v[i] = fmaf(-0.5f * fabsf(z), e, fmaxf(z, 0.f));
+      const float z = v[i], x = fabsf(z);
+      const float t = __builtin_amdgcn_rcpf(fmaf(x, 0.231641888f, 1.f));
+      float e = fmaf(t, 0.5307027145f, -0.7265760135f);
+      e = fmaf(t, e, 0.7107068705f);
+      e = fmaf(t, e, -0.142248368f);
+      e = fmaf(t, e, 0.127414796f) * t * __builtin_amdgcn_exp2f(-0.72134752f * x * x);
+      v[i] = fmaf(-fminf(x, 1e18f), e, fmaxf(z, 0.f));  // (infinity times 0 is none)
     }
   } else if (act == DARE_ACT_GELU_TANH) {
 #pragma unroll
@@ -1331,43 +1332,22 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
         }
       }
     } else {
+      // (LINEAR: the residual's rows a row of the tile ahead; columns behind the last one read the last ones, nobody stores them)
+      bf16x8 bias[LINEAR ? TN : 1], res[2][LINEAR ? TN : 1];
+      int at_col[LINEAR ? TN : 1];
+      auto residual = [&](int i) __attribute__((always_inline)) {
+        const bf16_t* row = p.residual + tok[i] * p.ldr;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) res[i & 1][j] = *reinterpret_cast<const bf16x8*>(row + at_col[j]);
+      };
       if constexpr (LINEAR) {
-        // (the residual's rows a row of the tile ahead; columns behind the last one read the last ones, nobody stores them)
-        bf16x8 bias[TN], res[2][TN];
-        int at_col[TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
           const int c = col0 + j * 32 + kq * 8;
           at_col[j] = c < n_end ? c : n_end - 8;
           if (p.bias) bias[j] = *reinterpret_cast<const bf16x8*>(p.bias + at_col[j]);
         }
-        auto residual = [&](int i) __attribute__((always_inline)) {
-          const bf16_t* row = p.residual + tok[i] * p.ldr;
-#pragma unroll
-          for (int j = 0; j < TN; ++j) res[i & 1][j] = *reinterpret_cast<const bf16x8*>(row + at_col[j]);
-        };
         if (p.residual) residual(0);
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-          if (p.residual && i + 1 < NA) residual(i + 1);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = value(i, j, e) + (p.bias ? (float)bias[j][e] : 0.f);
-            activate(p.act, v);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              f32x4 sum;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) sum[e] = v[4 * h + e] + (p.residual ? (float)res[i & 1][j][4 * h + e] : 0.f);
-              acc[i][2 * j + h] = sum;
-              asm volatile("" : "+a"(acc[i][2 * j + h]));
-            }
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
       if (!PART && !LINEAR && p.c32 && col0 < p.c32_cols) {
 #pragma unroll
@@ -1425,6 +1405,10 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
         const int other = from_half_row<0xf>(0, tok[i]);
         const bool live_other = from_half_row<0xf>(0, live[i]) != 0;
         const long own = tok[i] * ldc, far = other * ldc;
+        if constexpr (LINEAR) {
+          if (p.residual && i + 1 < NA) residual(i + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int j = 0; j < TN; j += 2) {
           u32x4 o[2];
@@ -1432,8 +1416,22 @@ __device__ __forceinline__ void gemm_tiles_quad(const GemmDev& p, const int m, u
           for (int h = 0; h < 2; ++h)
             if (j + h < TN) {
               bf16x8 r;
+              float v[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) r[e] = (bf16_t)value(i, j + h, e);
+              for (int e = 0; e < 8; ++e) v[e] = value(i, j + h, e);
+              if constexpr (LINEAR) {
+                if (p.bias) {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) v[e] += (float)bias[j + h][e];
+                }
+                activate(p.act, v);
+                if (p.residual) {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) v[e] += (float)res[i & 1][j + h][e];
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) r[e] = (bf16_t)v[e];
               o[h] = __builtin_bit_cast(u32x4, r);
             }
           bf16_t* to = base[j / 2];
@@ -1529,6 +1527,12 @@ __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsig
         if (!live) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) wf[u][e] = (bf16_t)0.0f;
+          if constexpr (LINEAR) {  // (0 times an infinity is none)
+#pragma unroll
+            for (int t = 0; t < TMS; ++t)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) xf[t][u][e] = (bf16_t)0.0f;
+          }
         }
       }
 #pragma unroll

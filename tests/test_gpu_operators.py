@@ -84,6 +84,10 @@ def test_linear_of_no_rows_and_special_values():
             assert out[0, 0] == x[0, 0] and out[2, 0] == x[2, 0]     # the identity far above 0, 0 far below
             assert abs(float(out[1, 0])) < 1e-30 and abs(float(out[3, 0])) < 1e-30
             assert torch.isnan(out[4, 0]) and not torch.isnan(out[5]).any()
+            y = x.clone()
+            y[4, 0], y[:4, 0] = float("inf"), 0.0
+            B.dare_k_linear(y, torch.ones(64, 64, dtype=dtype, device="cuda"), out, act=act)
+            assert (out[4] == float("inf")).all()
 
 
 # ---- rotary embedding -------------------------------------------------------------------------
