@@ -238,17 +238,34 @@ __global__ void __launch_bounds__(256) gemm_f32_kernel(GemmF32Dev p) {
 }
 
 template <int TM, int TN, int UNR>
-hipError_t launch_shape(const GemmF32Dev& p, bool linear, hipStream_t s) {
+hipError_t launch_shape(const GemmF32Dev& p, hipStream_t s) {
   constexpr int BM = 16 * TM, BN = 16 * TN;
   const int tm = (p.m_max + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
   if (tm == 0 || tn == 0) return hipSuccess;
-  if (linear)
-    hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, false, true>), dim3(tm, tn), dim3(256), 0, s, p);
-  else if (p.sel_mask)
+  if (p.sel_mask)
     hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, true>), dim3(tm, tn), dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, false>), dim3(tm, tn), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+
+// act(product + bias) + residual of all rows: the smallest tile that one round of the CUs is enough for, else the
+// largest that gives most of them one.  What bounds the small ones is the operands: 201 x 512 x 1536 in tiles of 16 x 16, 32 x 16 and 32 x 32 14.8,
+// 12.5, 16.4 us (8 waves or loads 8 steps ahead, 16 x 16: 15.0, 16.1), 100 x 768 x 768 8.6, 7.2, 9.3, 257 x 512 x 512 8.4, 8.7, 7.7, 128 x 256 x
+// 256 3.4, 4.1, 4.9, 300 x 1536 x 1536 33.6, 39.1, 29.2 (33.5 with loads 4 steps ahead).
+template <int TM, int TN, int UNR>
+hipError_t launch_linear_shape(const GemmF32Dev& p, hipStream_t s) {
+  const dim3 grid((p.m_max + 16 * TM - 1) / (16 * TM), (p.n + 16 * TN - 1) / (16 * TN));
+  hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, UNR, false, true>), grid, dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+hipError_t launch_linear(const GemmF32Dev& p, hipStream_t s) {
+  if (p.m_max == 0) return hipSuccess;
+  auto tiles = [&](int bm, int bn) { return (long)((p.m_max + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
+  if (tiles(16, 16) <= 256) return launch_linear_shape<1, 1, 4>(p, s);
+  if (tiles(32, 16) <= 256) return launch_linear_shape<2, 1, 4>(p, s);
+  if (tiles(64, 64) < 192) return launch_linear_shape<2, 2, 2>(p, s);
+  return launch_linear_shape<4, 4, 1>(p, s);
 }
 
 }  // namespace
@@ -286,15 +303,16 @@ hipError_t launch_gemm_f32(const GemmArgs& g, hipStream_t s) {
   p.ldr = g.ldr;
   p.act = g.act;
   if (p.sel_mask && (long)g.sel_batch * g.sel_seq > kSelMaxTokensF32) return hipErrorInvalidValue;
+  if (g.linear) return launch_linear(p, s);
   // The largest tile that gives most of the chip's 256 CUs a workgroup.  Measured (us; before: 64 x 64
   // tiles through LDS): 1024 x 12288 x 4096 1325 -> 880, 1024 x 2048 x 2048 141 -> 80 and
   // 514 x 3072 x 1024 74 -> 46, 32 x 126464 x 4096 920 -> 691, 205 refreshed of 1024 rows x 12288 x 4096 1095 ->
   // 925 (64 x 64), 64 x 4096 x 4096 235 -> 43 (32 x 32; 64 with 16 x 16, 84 with 64 x 64).
   auto tiles = [&](int b) { return (long)((g.m_max + b - 1) / b) * ((g.n + b - 1) / b); };
   constexpr long kFill = 192;
-  if (tiles(64) >= kFill) return launch_shape<4, 4, 1>(p, g.linear, s);
-  if (tiles(32) >= kFill) return launch_shape<2, 2, 4>(p, g.linear, s);
-  return launch_shape<1, 1, 4>(p, g.linear, s);
+  if (tiles(64) >= kFill) return launch_shape<4, 4, 1>(p, s);
+  if (tiles(32) >= kFill) return launch_shape<2, 2, 4>(p, s);
+  return launch_shape<1, 1, 4>(p, s);
 }
 
 }  // namespace dare

@@ -4,10 +4,16 @@
 // one launch: Q is rotated, K is rotated and stored at the token's cache row, V is stored there as it is.
 //
 // No table of angles: it would have to reach the largest position, and its rows are bytes that the
-// launch has to read.  A wave owns a token (or some of its heads); lane i takes cos and sin of pair i in 64
-// bits, where a position of 10^6 costs nothing of the angle's last bits in fp32, and leaves them to the other
-// lanes in LDS.
+// launch has to read.  A wave owns a token (or some of its heads); lane i takes cos and sin of pair i, the angle
+// formed and reduced to an eighth of a turn in 64 bits, where a position of 10^9 costs nothing of the last bits in fp32, and
+// leaves them to the other lanes in LDS.
+//
+// What bounds it: bytes where there are many tokens, latencies where there are few.  So a lane asks for its first kAtOnce items
+// before it turns to the angles, and few tokens are spread over as many waves as they have items for (rope_split).  us, 32 and 8 heads of
+// 128 channels, bf16, part by part with the angles first and now: 1 token 4.4 and 2.9, 8 4.8 and 3.0, 300 7.5 and 3.8,
+// 16384 81.2 and 82.8 (4.9 TB/s; a large copy reaches 5.0); 2, 4 and 8 items at once 82.8, 84.2, 83.1.
 #include "dare_common.h"
+#include "attn_packed.h"
 
 namespace dare {
 namespace {
@@ -16,7 +22,10 @@ struct RopeDev {
   const void* x[3];    // q, k, v
   void* out[3];
   long ldx[3], ldo[3]; // elements between tokens
-  int heads[3];        // 0: not there
+  // items of a token: chunks of its heads, 64 of a part in a turn of a wave; q's turns, then k's, then v's
+  int items[3], turns[3];  // turns: up to and including the part's
+  int per_head[3];
+  Divider by_per_head[3];
   int n, dim, rot;
   const int32_t* pos;
   const double* freqs;
@@ -25,7 +34,7 @@ struct RopeDev {
   float magnitude;
 };
 
-constexpr int kRopeWaves = 4;
+constexpr int kRopeWaves = 4, kAtOnce = 2;
 
 // V elements (of type E) that are read and written at once
 template <class E, int V>
@@ -33,97 +42,112 @@ struct alignas(V * sizeof(E) == 16 ? 16 : sizeof(E)) Chunk {
   E v[V];
 };
 
-// One token's part x (0 q, 1 k, 2 v) by the lanes of a wave: items `first`, first + step, ...  PAIRS: channels (2 i, 2 i + 1)
-// are a pair; else i and i + rot / 2.
+// PAIRS: channels (2 i, 2 i + 1) are a pair, an item is a chunk of V neighbouring channels.  Else i and i + rot / 2: an item is a chunk
+// of V channels i with the one of their partners, or a chunk of channels that are not rotated.
 template <class E, int V, bool PAIRS>
-__device__ __forceinline__ void rope_part(const E* x, E* out, int heads, int dim, int rot, const float* cs, bool turns,
-                                          int first, int step) {
+__global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
   typedef Chunk<E, V> chunk_t;
-  const int half = rot >> 1;
-  if (!turns || PAIRS) {
-    // whole chunks of neighbouring channels
-    const int per_head = dim / V, items = heads * per_head;
-    for (int it = first; it < items; it += step) {
-      const int u = it % per_head;
-      chunk_t c = reinterpret_cast<const chunk_t*>(x)[it];
-      if constexpr (PAIRS && V > 1) {
-        if (turns) {
+  __shared__ float cs_all[kRopeWaves][kRopeMaxDim];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long t = (long)blockIdx.x * kRopeWaves + wave;
+  if (t >= p.n) return;  // (no barrier below: a wave reads what its own lanes wrote)
+  float* cs = cs_all[wave];
+  const int half = p.rot >> 1, step = gridDim.y;
+  const int position = p.pos[t], row = p.rows ? p.rows[t] : t;
+  const bool stored = !p.rows || (row >= 0 && row < p.out_rows);  // k and v of this token
+
+  for (int w0 = blockIdx.y; w0 < p.turns[2]; w0 += kAtOnce * step) {
+    chunk_t a[kAtOnce], b[kAtOnce];
+    E* base[kAtOnce];   // the part's output row (the same in all lanes)
+    int at[kAtOnce];    // the item's first channel in it, -1: no item
+    int pair[kAtOnce];  // number of the item's first pair, -1 if none of its channels is rotated
 #pragma unroll
-          for (int e = 0; e < V; e += 2) {
-            const int i = (u * V + e) >> 1;
-            if (i < half) {
-              const float a = (float)c.v[e], b = (float)c.v[e + 1], co = cs[2 * i], si = cs[2 * i + 1];
-              c.v[e] = (E)(a * co - b * si);
-              c.v[e + 1] = (E)(b * co + a * si);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int w = w0 + i * step;
+      at[i] = pair[i] = -1;
+      const int part = w < p.turns[0] ? 0 : w < p.turns[1] ? 1 : 2;
+      if (w >= p.turns[2] || (part > 0 && !stored)) continue;
+      const E* src = static_cast<const E*>(p.x[part]) + t * p.ldx[part];
+      base[i] = static_cast<E*>(p.out[part]) + (part == 0 ? t : row) * p.ldo[part];
+      const int item = (w - (part == 0 ? 0 : p.turns[part - 1])) * 64 + lane;
+      if (item >= p.items[part]) continue;
+      const int head = divide(item, p.by_per_head[part]), u = item - head * p.per_head[part];
+      int c = u * V;      // first channel
+      bool turns = part < 2 && c < p.rot;
+      if (!PAIRS && part < 2) {
+        turns = c < half;
+        c += turns ? 0 : half;
+      }
+      at[i] = head * p.dim + c;
+      a[i] = *reinterpret_cast<const chunk_t*>(src + at[i]);
+      if (turns) {
+        pair[i] = PAIRS ? c >> 1 : c;
+        if (!PAIRS) b[i] = *reinterpret_cast<const chunk_t*>(src + at[i] + half);
+      }
+    }
+    if (w0 == (int)blockIdx.y) {
+      __builtin_amdgcn_sched_barrier(0);
+      for (int i = lane; i < half; i += 64) {
+        const double x = (double)position * p.freqs[i] * 0.318309886183790671538;  // half turns
+        const double quarter = rint(2.0 * x);
+        float s, c;
+        sincospif((float)(x - 0.5 * quarter), &s, &c);
+        const int q = (int)(quarter - 4.0 * floor(0.25 * quarter));
+        const float co = q & 1 ? s : c, si = q & 1 ? c : s;
+        cs[2 * i] = (q == 1 || q == 2 ? -co : co) * p.magnitude;
+        cs[2 * i + 1] = (q >= 2 ? -si : si) * p.magnitude;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (at[i] < 0) continue;
+      if (PAIRS) {
+        if (V > 1 && pair[i] >= 0) {
+#pragma unroll
+          for (int e = 0; e + 1 < V; e += 2) {
+            const int j = pair[i] + (e >> 1);
+            if (j < half) {
+              const float x = (float)a[i].v[e], y = (float)a[i].v[e + 1], co = cs[2 * j], si = cs[2 * j + 1];
+              a[i].v[e] = (E)(x * co - y * si);
+              a[i].v[e + 1] = (E)(y * co + x * si);
             }
           }
         }
-      }
-      reinterpret_cast<chunk_t*>(out)[it] = c;
-    }
-    return;
-  }
-  // chunk u < half / V with its partner half channels on; behind them the channels that are not rotated
-  const int turning = half / V, per_head = turning + (dim - rot) / V, items = heads * per_head;
-  for (int it = first; it < items; it += step) {
-    const int h = it / per_head, u = it - h * per_head;
-    const E* src = x + (long)h * dim;
-    E* dst = out + (long)h * dim;
-    if (u < turning) {
-      chunk_t a = *reinterpret_cast<const chunk_t*>(src + u * V), b = *reinterpret_cast<const chunk_t*>(src + half + u * V);
+      } else if (pair[i] >= 0) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float co = cs[2 * (u * V + e)], si = cs[2 * (u * V + e) + 1];
-        const float p = (float)a.v[e], q = (float)b.v[e];
-        a.v[e] = (E)(p * co - q * si);
-        b.v[e] = (E)(q * co + p * si);
+        for (int e = 0; e < V; ++e) {
+          const float co = cs[2 * (pair[i] + e)], si = cs[2 * (pair[i] + e) + 1];
+          const float x = (float)a[i].v[e], y = (float)b[i].v[e];
+          a[i].v[e] = (E)(x * co - y * si);
+          b[i].v[e] = (E)(y * co + x * si);
+        }
+        *reinterpret_cast<chunk_t*>(base[i] + at[i] + half) = b[i];
       }
-      *reinterpret_cast<chunk_t*>(dst + u * V) = a;
-      *reinterpret_cast<chunk_t*>(dst + half + u * V) = b;
-    } else {
-      const int c = rot + (u - turning) * V;
-      *reinterpret_cast<chunk_t*>(dst + c) = *reinterpret_cast<const chunk_t*>(src + c);
+      *reinterpret_cast<chunk_t*>(base[i] + at[i]) = a[i];
     }
   }
 }
 
-// gridDim.y workgroups share the heads of a token between them
-template <class E, int V, bool PAIRS>
-__global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
-  __shared__ float cs_all[kRopeWaves][kRopeMaxDim];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = blockIdx.x * kRopeWaves + wave;
-  if (t >= p.n) return;  // (no barrier below: a wave reads what its own lanes wrote)
-  float* cs = cs_all[wave];
-  const double position = (double)p.pos[t];
-  for (int i = lane; i < p.rot >> 1; i += 64) {
-    double s, c;
-    sincospi(position * p.freqs[i] * 0.318309886183790671538, &s, &c);
-    cs[2 * i] = (float)(c * p.magnitude);
-    cs[2 * i + 1] = (float)(s * p.magnitude);
-  }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  const int first = blockIdx.y * 64 + lane, step = gridDim.y * 64;
-  const long row = p.rows ? (long)p.rows[t] : t;
-#pragma unroll
-  for (int part = 0; part < 3; ++part) {
-    if (p.heads[part] == 0) continue;
-    long to = t;
-    if (part > 0 && p.rows) {
-      if (row < 0 || row >= p.out_rows) continue;
-      to = row;
-    }
-    rope_part<E, V, PAIRS>(static_cast<const E*>(p.x[part]) + t * p.ldx[part], static_cast<E*>(p.out[part]) + to * p.ldo[part],
-                           p.heads[part], p.dim, p.rot, cs, part < 2, first, step);
-  }
+// Workgroups that share a token's turns: 4096 waves in all where there are turns for them
+int rope_split(int n, int turns) {
+  const int want = n < 4096 ? 4096 / n : 1;
+  return want < turns ? want : turns;
 }
 
 // V: elements at once where that is possible; NARROW: channel by channel, or pair by pair where they are neighbours
 template <class E, int V, bool NARROW>
-hipError_t launch_layout(const RopeDev& p, bool pairs, hipStream_t s) {
-  const dim3 grid((p.n + kRopeWaves - 1) / kRopeWaves, 1), block(kRopeWaves * 64);
+hipError_t launch_layout(RopeDev p, const int (&heads)[3], bool pairs, hipStream_t s) {
+  const int v = !NARROW ? V : pairs ? 2 : 1;
+  for (int i = 0, end = 0; i < 3; ++i) {
+    p.per_head[i] = !pairs && i < 2 ? p.rot / 2 / v + (p.dim - p.rot) / v : p.dim / v;
+    p.by_per_head[i] = divider(p.per_head[i]);
+    p.items[i] = heads[i] * p.per_head[i];
+    p.turns[i] = end += (p.items[i] + 63) / 64;
+  }
+  const dim3 grid((p.n + kRopeWaves - 1) / kRopeWaves, rope_split(p.n, p.turns[2])), block(kRopeWaves * 64);
   if (pairs)
     hipLaunchKernelGGL((rope_kernel<E, NARROW ? 2 : V, true>), grid, block, 0, s, p);
   else
@@ -138,13 +162,14 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s) {
   RopeDev p{};
   const size_t esize = dtype == DARE_BF16 ? 2 : 4;
   uintptr_t bits = 0;  // of everything that has to be a multiple of 16 bytes
+  int heads[3];
   for (int i = 0; i < 3; ++i) {
     p.x[i] = a.x[i];
     p.out[i] = a.out[i];
     p.ldx[i] = a.ldx[i];
     p.ldo[i] = a.ldo[i];
-    p.heads[i] = a.x[i] ? a.heads[i] : 0;
-    if (p.heads[i]) bits |= (uintptr_t)a.x[i] | (uintptr_t)a.out[i] | a.ldx[i] * esize | a.ldo[i] * esize;
+    heads[i] = a.x[i] ? a.heads[i] : 0;
+    if (heads[i]) bits |= (uintptr_t)a.x[i] | (uintptr_t)a.out[i] | a.ldx[i] * esize | a.ldo[i] * esize;
   }
   p.n = a.n;
   p.dim = a.dim;
@@ -154,12 +179,12 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s) {
   p.rows = a.rows;
   p.out_rows = a.out_rows;
   p.magnitude = a.magnitude;
-  // 16 bytes at a time where everything lies on such a boundary and, by halves, a chunk has its partner in one chunk
+  // 16 bytes at a time where everything lies on such a boundary and, by halves, a chunk has its partners in one chunk
   const int v = (int)(16 / esize);
   const bool wide = bits % 16 == 0 && a.dim % v == 0 && (a.pairs || (a.rot / 2) % v == 0);
   if (dtype == DARE_BF16)
-    return wide ? launch_layout<bf16_t, 8, false>(p, a.pairs, s) : launch_layout<bf16_t, 8, true>(p, a.pairs, s);
-  return wide ? launch_layout<float, 4, false>(p, a.pairs, s) : launch_layout<float, 4, true>(p, a.pairs, s);
+    return wide ? launch_layout<bf16_t, 8, false>(p, heads, a.pairs, s) : launch_layout<bf16_t, 8, true>(p, heads, a.pairs, s);
+  return wide ? launch_layout<float, 4, false>(p, heads, a.pairs, s) : launch_layout<float, 4, true>(p, heads, a.pairs, s);
 }
 
 }  // namespace dare
