@@ -49,11 +49,9 @@ constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, i
   plan.blocks = (int)((long)total_q * group / plan.rows) + batch;
   plan.parts = 1;
   plan.part_keys = 1 << 30;
-  // Few rows: parts of 512 keys, the unit that keeps a CU busy for longer than a workgroup takes to start and to end (384
-  // and 768: one token over each of 64 sequences of 500 to 8000 keys, 32 and 8 heads, 169 and 161 us for 159, over 32 of 40 to 4000 38 and
-  // 37 for 35); shorter ones, down to 128, where those do not give every CU two workgroups (8 sequences of 1000 keys: parts of 1000, 500
-  // and 128 25, 19 and 16 us); longer ones where there would be more than 64, or more than 16 rounds of workgroups, which even
-  // out by themselves.
+  // Few rows: parts of 128 keys and more (Layout in attn_packed_rows.h takes what it needs of them), where there are 512 keys to cut
+  // (8 sequences of 300 keys uncut 10.6 us, in two parts 12.0), and fewer where 16 rounds of workgroups even out by themselves.  For
+  // more than 256 sequences, whose lengths a workgroup does not look through, parts of 512.
   // Many rows, whose partial results are bytes that count: as many parts as give every CU two workgroups, or, up to four, four, because
   // sequences differ and masked rows see less (32 tokens each over 32 caches of 100 to 4000 keys 98 us with two parts, 79 with
   // four, 2000 causal ones 45 and 41, but 64 over 60000 keys 96 with 32 parts and 120 with 64); of 512 keys, or 256 where
@@ -63,8 +61,9 @@ constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, i
   const long pairs = (filled > some ? filled : some > 0 ? some : 1) * n_kv;
   long room = 8192 / pairs;
   if (plan.rows == 128) room = 512 / pairs >= 4 ? 512 / pairs : 1024 / pairs < 4 ? 1024 / pairs : 4;
-  const long even = max_k * pairs / 512, least = plan.rows == 128 ? 256 : 128;
-  long parts = max_k / (even > 512 ? 512 : even > least ? even : least);
+  const long even = max_k * pairs / 512;
+  long parts = max_k / (plan.rows < 128 || even > 512 ? 512 : even > 256 ? even : 256);
+  if (plan.rows < 128 && batch <= 256 && parts > 0) parts = max_k / 128;
   if (parts > room) parts = room;
   if (parts > kPackedMaxParts) parts = kPackedMaxParts;
   if (parts > 1) {

@@ -257,27 +257,25 @@ __device__ __forceinline__ float* part_slot(const PackedDev& p, int g, int kvh, 
 // ---- few rows: 16 R of them, the keys shared by the waves -----------------------------------------
 // Every wave takes every second (heads of 64 channels: fourth) tile of 32 keys through two stages of its own, so that the waves meet at
 // the end only.  64 KB of stages per workgroup, two workgroups on a CU: one reads while the other starts or ends.
-constexpr int kFewKeys = 32;
+constexpr int kFewKeys = 32, kFewSlots = 512;
 template <int DH>
 constexpr int kFewWaves = DH == 128 ? 2 : 4;
 
 template <int DH, int R>
-__global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(PackedDev p) {
+struct FewShared {
+  unsigned char stages[kFewWaves<DH> * 4 * kFewKeys * DH * 2];
+  float m[kFewWaves<DH>][R][16], l[kFewWaves<DH>][R][16];
+};
+
+// Tiles [first, last) of the keys of a block; slot: where a part's results go, nullptr if the block has one part
+template <int DH, int R>
+__device__ __forceinline__ void few_rows(const PackedDev& p, const Place& at, int kvh, int first, int last, float* slot,
+                                         FewShared<DH, R>& shared) {
   constexpr int BM = 16 * R, CB = DH / 16, TILE = kFewKeys * DH * 2, STAGE = 2 * TILE, L = TILE / 1024, NW = kFewWaves<DH>;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 2 * STAGE];
-  __shared__ float m_all[NW][R][16], l_all[NW][R][16];
+  unsigned char* const smem = shared.stages;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kq = lane >> 4;
-  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
-  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
-  Place at;
-  if (!find_block<BM>(p.rows, g, at)) return;
-
-  const int least = row_limit(p.rows, at, at.row0), most = row_limit(p.rows, at, at.row0 + at.rows - 1);
-  const int tiles = (most + kFewKeys - 1) / kFewKeys, n_parts = parts_of(p, tiles);
-  if (part >= n_parts) return;
-  const int first = (int)((long)tiles * part / n_parts), last = (int)((long)tiles * (part + 1) / n_parts);
-
+  const int least = row_limit(p.rows, at, at.row0);  // keys that all rows see
   const bf16_t* kbase = p.k + (long)at.k0 * p.ldk + kvh * DH;
   const bf16_t* vbase = p.v + (long)at.k0 * p.ldv + kvh * DH;
   const unsigned lds0 = (unsigned)(size_t)(lptr_t)smem + wave * 2 * STAGE;
@@ -325,8 +323,8 @@ __global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(Pac
   for (int r = 0; r < R; ++r) {
     const float l = row_sum(w.l[r]);
     if (kq == 0) {
-      m_all[wave][r][l16] = w.m[r];
-      l_all[wave][r][l16] = l;
+      shared.m[wave][r][l16] = w.m[r];
+      shared.l[wave][r][l16] = l;
     }
 #pragma unroll
     for (int c = 0; c < CB; ++c) reinterpret_cast<f32x4*>(mine)[(c * R + r) * 64 + lane] = w.acc[c][r];
@@ -335,13 +333,13 @@ __global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(Pac
   constexpr int OWN = CB / NW;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    float m = m_all[0][r][l16], l = 0.f, f[NW];
+    float m = shared.m[0][r][l16], l = 0.f, f[NW];
 #pragma unroll
-    for (int o = 1; o < NW; ++o) m = fmaxf(m, m_all[o][r][l16]);
+    for (int o = 1; o < NW; ++o) m = fmaxf(m, shared.m[o][r][l16]);
 #pragma unroll
     for (int o = 0; o < NW; ++o) {
-      f[o] = __builtin_amdgcn_exp2f(m_all[o][r][l16] - m);
-      l += l_all[o][r][l16] * f[o];
+      f[o] = __builtin_amdgcn_exp2f(shared.m[o][r][l16] - m);
+      l += shared.l[o][r][l16] * f[o];
     }
     const int row = r * 16 + l16;
     if (row >= at.rows) continue;
@@ -354,8 +352,7 @@ __global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(Pac
       for (int o = 0; o < NW; ++o)
         sum[i] += reinterpret_cast<const f32x4*>(smem + o * 2 * STAGE)[(c * R + r) * 64 + lane] * f[o];
     }
-    if (n_parts > 1) {
-      float* slot = part_slot<DH, BM>(p, g, kvh, part);
+    if (slot) {
 #pragma unroll
       for (int i = 0; i < OWN; ++i) *reinterpret_cast<f32x4*>(slot + row * DH + (wave * OWN + i) * 16 + kq * 4) = sum[i];
       if (wave == 0 && kq == 0) {
@@ -373,6 +370,41 @@ __global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(Pac
       }
     }
   }
+}
+
+// Up to 64 S sequences: as many workgroups as run at once walk over what there is to do.  (A workgroup for every part that
+// there might be, as with more sequences: those without one take 64 KB of LDS and 1.5 us each before they are gone; one token over
+// each of 32 caches of 40 to 4000 keys 33.7 us and in this form 30.1, of 4 of 32000 111 and 100, of 64 of 500 to 8000 158 and 149.)
+template <int DH, int R, int S>
+__global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(PackedDev p) {
+  __shared__ __attribute__((aligned(1024))) FewShared<DH, R> shared;
+  Layout<16 * R, kFewKeys, S> all;
+  all.read(p.rows, p.n_kv, kFewSlots, p.max_parts);
+  for (int u = blockIdx.x; u < all.n_units * p.n_kv; u += gridDim.x) {
+    const int kvh = u % p.n_kv;
+    Place at;
+    int block, part, n_parts;
+    all.unit(p.rows, u / p.n_kv, at, block, part, n_parts);
+    // (offsets that do not ascend can lead anywhere)
+    if (at.row0 < 0 || at.rows <= 0 || (unsigned)block >= (unsigned)p.rows.n_blocks || (unsigned)part >= (unsigned)n_parts) continue;
+    const int tiles = (row_limit(p.rows, at, at.row0 + at.rows - 1) + kFewKeys - 1) / kFewKeys;
+    if (u != (int)blockIdx.x) __syncthreads();  // the stages are used again
+    few_rows<DH, R>(p, at, kvh, (int)((long)tiles * part / n_parts), (int)((long)tiles * (part + 1) / n_parts),
+                    n_parts > 1 ? part_slot<DH, 16 * R>(p, block, kvh, part) : nullptr, shared);
+  }
+}
+
+template <int DH, int R>
+__global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_searched_kernel(PackedDev p) {
+  __shared__ __attribute__((aligned(1024))) FewShared<DH, R> shared;
+  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
+  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
+  Place at;
+  if (!find_block<16 * R>(p.rows, g, at)) return;
+  const int tiles = (row_limit(p.rows, at, at.row0 + at.rows - 1) + kFewKeys - 1) / kFewKeys, n_parts = parts_of(p, tiles);
+  if (part >= n_parts) return;
+  few_rows<DH, R>(p, at, kvh, (int)((long)tiles * part / n_parts), (int)((long)tiles * (part + 1) / n_parts),
+                  n_parts > 1 ? part_slot<DH, 16 * R>(p, g, kvh, part) : nullptr, shared);
 }
 
 // ---- many rows: 128 of them, four waves of 32 rows on the same keys --------------------------------
@@ -706,15 +738,6 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
 
 // ---- parts of a row's keys, joined ---------------------------------------------------------------
 // What bounds both forms is the latency of what other XCDs have written; so all that a row needs is asked for at once.
-// The row (and its block) of a lane's token; false without one, or with one part
-template <int DH, int BM, int KEYS>
-__device__ __forceinline__ bool join_place(const PackedDev& p, int row, Place& at, const float*& slot, int& n_parts) {
-  const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
-  if (!find_block<BM>(p.rows, g, at) || row >= at.rows) return false;
-  n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + KEYS - 1) / KEYS);
-  slot = part_slot<DH, BM>(p, g, kvh, 0);
-  return n_parts > 1;
-}
 // channels c .. c + 3 of the row
 __device__ __forceinline__ void join_store(const PackedDev& p, const Place& at, int row, int c, int dh, f32x4 sum, float l) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -728,15 +751,27 @@ __device__ __forceinline__ void join_store(const PackedDev& p, const Place& at, 
 
 // Few rows, up to 64 parts: a wave per row.  Lane q holds the reference and the sum of part q; DH / 4 lanes hold a part's channels, so
 // 2 (4) parts are read side by side, eight times that many at once.
-template <int DH, int BM>
+// S: sequences per lane of the layout, 0 where the blocks were searched.
+template <int DH, int BM, int S>
 __global__ void __launch_bounds__(256) attn_packed_join_few_kernel(PackedDev p) {
   constexpr int LANES = DH / 4, SIDE = 64 / LANES, AT_ONCE = 8;
   constexpr long SLOT = packed_slot_floats(DH, BM);
   const int lane = threadIdx.x & 63, row = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Place at;
-  const float* slot;
   int n_parts;
-  if (!join_place<DH, BM, kFewKeys>(p, row, at, slot, n_parts)) return;
+  const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
+  if constexpr (S > 0) {
+    Layout<BM, kFewKeys, S> all;
+    all.read(p.rows, p.n_kv, kFewSlots, p.max_parts);
+    if (g >= all.n_blocks) return;
+    all.block(p.rows, g, at, n_parts);
+    if (at.row0 < 0) return;
+  } else {
+    if (!find_block<BM>(p.rows, g, at)) return;
+    n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + kFewKeys - 1) / kFewKeys);
+  }
+  if (row >= at.rows || n_parts < 2) return;
+  const float* slot = part_slot<DH, BM>(p, g, kvh, 0);
   const int own = lane < n_parts ? lane : n_parts - 1, c = lane % LANES * 4, side = lane / LANES;
   const float m_own = slot[own * SLOT + BM * DH + row], l_own = slot[own * SLOT + BM * DH + BM + row];
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -777,9 +812,11 @@ __global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p)
   constexpr long SLOT = packed_slot_floats(DH, BM);
   const int row = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
   Place at;
-  const float* slot;
-  int n_parts;
-  if (!join_place<DH, BM, kManyKeys>(p, row, at, slot, n_parts)) return;
+  const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
+  if (!find_block<BM>(p.rows, g, at) || row >= at.rows) return;
+  const int n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys);
+  if (n_parts < 2) return;
+  const float* slot = part_slot<DH, BM>(p, g, kvh, 0);
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   float m = -__FLT_MAX__, l = 0.f;
   for (int q0 = 0; q0 < n_parts; q0 += AT_ONCE) {
@@ -810,13 +847,24 @@ __global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p)
   join_store(p, at, row, c, DH, sum, l);
 }
 
-template <int DH, int R>
-hipError_t launch_few(PackedDev p, const PackedPlan& plan, hipStream_t s) {
-  const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
-  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R>), grid, dim3(kFewWaves<DH> * 64), 0, s, p);
+template <int DH, int R, int S>
+hipError_t launch_few_laid(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  const long most = (long)plan.blocks * plan.parts * p.n_kv;
+  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R, S>), dim3((unsigned)(most < kFewSlots ? most : kFewSlots)), dim3(kFewWaves<DH> * 64), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.parts == 1) return e;
-  hipLaunchKernelGGL((attn_packed_join_few_kernel<DH, 16 * R>), dim3((unsigned)(plan.blocks * p.n_kv), 4 * R), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((attn_packed_join_few_kernel<DH, 16 * R, S>), dim3((unsigned)(plan.blocks * p.n_kv), 4 * R), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+template <int DH, int R>
+hipError_t launch_few(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  if (p.rows.batch <= 64) return launch_few_laid<DH, R, 1>(p, plan, s);
+  if (p.rows.batch <= 256) return launch_few_laid<DH, R, 4>(p, plan, s);
+  const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
+  hipLaunchKernelGGL((attn_packed_few_searched_kernel<DH, R>), grid, dim3(kFewWaves<DH> * 64), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.parts == 1) return e;
+  hipLaunchKernelGGL((attn_packed_join_few_kernel<DH, 16 * R, 0>), dim3((unsigned)(plan.blocks * p.n_kv), 4 * R), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -70,6 +70,138 @@ __device__ __forceinline__ bool find_block(const PackedRows& p, const int g, Pla
   return true;
 }
 
+// Inclusive sum along the lanes
+__device__ __forceinline__ int wave_prefix_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8: within 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15: lane 15 to row 1, 47 to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast 31: lane 31 to rows 2 and 3
+  return v;
+}
+
+// All sequences of a launch (64 S at most), S in each lane: their blocks of BM rows and the parts that the keys of a block (tiles of
+// KEYS) are cut into, by the lengths as they are and not as the host knows them, without a number for a block or a part that is not there.
+// Blocks are numbered by lane, then by sequence of the lane.
+template <int BM, int KEYS, int S>
+struct Layout {
+  int q0[S], len_q[S], k0[S], len_k[S], blocks[S], parts[S];
+  int blocks_upto, units_upto;  // of the lanes up to and including this one
+  int n_blocks, n_units;        // in all
+
+  // slots: workgroups that run at once.  A part is what makes about as many parts as there are slots (with many blocks, four for every
+  // block), each block's last one half full; 4 tiles at least.
+  __device__ __forceinline__ void read(const PackedRows& p, int n_kv, int slots, int max_parts) {
+    const int lane = threadIdx.x & 63;
+    int begin[S], stop[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int b = lane + 64 * i < p.batch ? lane + 64 * i : p.batch - 1;
+      q0[i] = p.q_off[b];
+      len_q[i] = p.q_off[b + 1];
+      begin[i] = p.k_begin[b];
+      stop[i] = p.k_end[b];
+    }
+    auto within = [](int v, int end) __attribute__((always_inline)) { return v < 0 ? 0 : v > end ? end : v; };
+    float work = 0.f;
+    int own_blocks = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      q0[i] = within(q0[i], p.total_q);
+      const int n = within(len_q[i], p.total_q) - q0[i];
+      len_q[i] = lane + 64 * i < p.batch && n > 0 ? n : 0;
+      k0[i] = within(begin[i], p.k_rows);
+      const int m = within(stop[i], p.k_rows) - k0[i];
+      len_k[i] = m > 0 ? m : 0;
+      blocks[i] = (int)((unsigned)(len_q[i] * p.group + BM - 1) / BM);
+      own_blocks += blocks[i];
+      work += (float)blocks[i] * (float)((unsigned)len_k[i] / KEYS + 1);
+    }
+    blocks_upto = wave_prefix_sum(own_blocks);
+    n_blocks = __builtin_amdgcn_readlane(blocks_upto, 63);
+    int part_tiles = 1 << 30;
+    if (max_parts > 1) {
+      const float pairs = (float)n_blocks * (float)n_kv, wanted = pairs <= 0.5f * (float)slots ? (float)slots : 4.f * pairs;
+      part_tiles = (int)(wave_sum(work) * (float)n_kv / (wanted - 0.5f * pairs)) + 1;
+      part_tiles = __builtin_amdgcn_readfirstlane(part_tiles < 4 ? 4 : part_tiles);
+    }
+    int own_units = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int tiles = (int)(((unsigned)len_k[i] + KEYS - 1) / KEYS);
+      const int n = (tiles + part_tiles - 1) / part_tiles;
+      parts[i] = n < 1 ? 1 : n < max_parts ? n : max_parts;
+      own_units += blocks[i] * parts[i];
+    }
+    units_upto = wave_prefix_sum(own_units);
+    n_units = __builtin_amdgcn_readlane(units_upto, 63);
+  }
+
+  // Place of block `local` of sequence i of lane l
+  __device__ __forceinline__ void place(const PackedRows& p, int l, int i, int local, Place& at, int& n_parts) const {
+#pragma unroll
+    for (int j = 0; j < S; ++j)
+      if (j == i) {
+        at.q0 = __builtin_amdgcn_readlane(q0[j], l);
+        at.k0 = __builtin_amdgcn_readlane(k0[j], l);
+        at.len_k = __builtin_amdgcn_readlane(len_k[j], l);
+        const int len = __builtin_amdgcn_readlane(len_q[j], l), rows = len * p.group - local * BM;
+        at.shift = at.len_k - len;
+        at.row0 = local * BM;
+        at.rows = rows < BM ? rows : BM;
+        n_parts = __builtin_amdgcn_readlane(parts[j], l);
+      }
+  }
+  // Unit u < n_units: its place, number of the block, part
+  __device__ __forceinline__ void unit(const PackedRows& p, int u, Place& at, int& block, int& part, int& n_parts) const {
+    const int l = __builtin_ctzll(__ballot(units_upto > u));
+    int own = 0, b = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      own += blocks[i] * parts[i];
+      b += blocks[i];
+    }
+    u -= __builtin_amdgcn_readlane(units_upto - own, l);
+    block = __builtin_amdgcn_readlane(blocks_upto - b, l);
+    int i = 0, local = 0;
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const int here = __builtin_amdgcn_readlane(blocks[j], l), cut = __builtin_amdgcn_readlane(parts[j], l);
+      if (i == j) {
+        if (u >= here * cut && j + 1 < S) {
+          u -= here * cut;
+          block += here;
+          i = j + 1;
+        } else {
+          local = u / cut;
+          part = u - local * cut;
+        }
+      }
+    }
+    block += local;
+    place(p, l, i, local, at, n_parts);
+  }
+  // Block c < n_blocks
+  __device__ __forceinline__ void block(const PackedRows& p, int c, Place& at, int& n_parts) const {
+    const int l = __builtin_ctzll(__ballot(blocks_upto > c));
+    int b = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) b += blocks[i];
+    c -= __builtin_amdgcn_readlane(blocks_upto - b, l);
+    int i = 0;
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+      const int here = __builtin_amdgcn_readlane(blocks[j], l);
+      if (i == j && c >= here && j + 1 < S) {
+        c -= here;
+        i = j + 1;
+      }
+    }
+    place(p, l, i, c, at, n_parts);
+  }
+};
+
 // Keys that row j of the sequence sees
 __device__ __forceinline__ int row_limit(const PackedRows& p, const Place& at, int j) {
   return packed_limit(divide(j, p.by_group), at.shift, at.len_k, p.causal_block, p.by_causal_block);
