@@ -38,7 +38,8 @@ struct PackedDev {
   PackedRows rows;
   int n_kv;
   int max_parts;    // parts launched per block; with one part there is no workspace
-  int part_tiles;   // tiles of a part, at least
+  int part_tiles;   // tiles of a part, at least (more than 256 sequences)
+  int slots;        // workgroups that parts are made for (up to 256 sequences)
   float* parts;     // [block][key head][part] partial results
   float scale_log2;
 };
@@ -257,7 +258,7 @@ __device__ __forceinline__ float* part_slot(const PackedDev& p, int g, int kvh, 
 // ---- few rows: 16 R of them, the keys shared by the waves -----------------------------------------
 // Every wave takes every second (heads of 64 channels: fourth) tile of 32 keys through two stages of its own, so that the waves meet at
 // the end only.  64 KB of stages per workgroup, two workgroups on a CU: one reads while the other starts or ends.
-constexpr int kFewKeys = 32, kFewSlots = 512;
+constexpr int kFewKeys = 32;
 template <int DH>
 constexpr int kFewWaves = DH == 128 ? 2 : 4;
 
@@ -378,8 +379,8 @@ __device__ __forceinline__ void few_rows(const PackedDev& p, const Place& at, in
 template <int DH, int R, int S>
 __global__ void __launch_bounds__(kFewWaves<DH> * 64) attn_packed_few_kernel(PackedDev p) {
   __shared__ __attribute__((aligned(1024))) FewShared<DH, R> shared;
-  Layout<16 * R, kFewKeys, S> all;
-  all.read(p.rows, p.n_kv, kFewSlots, p.max_parts);
+  Layout<16 * R, kFewKeys, S, false> all;
+  all.read(p.rows, p.n_kv, p.slots, p.max_parts);
   for (int u = blockIdx.x; u < all.n_units * p.n_kv; u += gridDim.x) {
     const int kvh = u % p.n_kv;
     Place at;
@@ -423,7 +424,15 @@ __device__ __forceinline__ void wait_vmcnt_and_barrier() {
 }
 
 template <int DH>
-__global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(PackedDev p) {
+struct ManyShared {
+  unsigned char stages[4 * kManyKeys * DH * 2];
+  long out_rows[kManyRows];  // where the rows' outputs lie
+};
+
+// Steps (tiles of the keys) [first, first + n_steps) of a block; slot: where a part's results go, nullptr if the block has one part
+template <int DH>
+__device__ __forceinline__ void many_rows(const PackedDev& p, const Place& at, int kvh, const int first, const int n_steps, float* slot,
+                                          ManyShared<DH>& shared) {
   constexpr int BM = kManyRows, CB = DH / 16, ROWB = DH * 2, TILE = kManyKeys * ROWB;
   constexpr int CPR = DH / 8, RPL = 64 / CPR;      // 16-byte chunks per row, rows of a wave's load
   constexpr int KL = TILE / 1024 / kManyWaves;     // a wave's loads of K (or V) per step
@@ -434,21 +443,10 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   using No = std::false_type;
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];
-  __shared__ long out_rows[BM];  // where the rows' outputs lie
-
+  unsigned char* const smem = shared.stages;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kq = lane >> 4;
-  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
-  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
-  Place at;
-  if (!find_block<BM>(p.rows, g, at)) return;
-
-  // steps of the block's part, and of them the wave's: those that all of its rows see whole, those that one of them sees
-  const int most = row_limit(p.rows, at, at.row0 + at.rows - 1);
-  const int tiles = (most + kManyKeys - 1) / kManyKeys, n_parts = parts_of(p, tiles);
-  if (part >= n_parts) return;
-  const int first = (int)((long)tiles * part / n_parts), n_steps = (int)((long)tiles * (part + 1) / n_parts) - first;
+  // of the steps the wave's: those that all of its rows see whole, those that one of them sees
   const bool any_row = wave * 32 < at.rows;  // (a wave without rows only loads)
   int whole = 0, mine = 0, ends = 0;  // ends: keys that the wave's last row sees
   if (any_row) {
@@ -512,7 +510,7 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   w.clear();
   if (kq == 0) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) out_rows[wave * 32 + r * 16 + l16] = out_at[r];
+    for (int r = 0; r < 2; ++r) shared.out_rows[wave * 32 + r * 16 + l16] = out_at[r];
   }
 
   // ---- fragments ----
@@ -696,17 +694,15 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   float l[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r) l[r] = row_sum(w.l[r]);
-  if (n_parts > 1) {
-    float* slot = part_slot<DH, BM>(p, g, kvh, part);
+  if (slot) {  // (as the sums lie in the lanes: whole kilobytes)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int row = wave * 32 + r * 16 + l16;
-      if (row >= at.rows) continue;
+      if (wave * 32 + r * 16 >= at.rows) break;
 #pragma unroll
-      for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4*>(slot + row * DH + c * 16 + kq * 4) = w.acc[c][r];
+      for (int c = 0; c < CB; ++c) reinterpret_cast<f32x4*>(slot)[((wave * CB + c) * 2 + r) * 64 + lane] = w.acc[c][r];
       if (kq == 0) {
-        slot[BM * DH + row] = w.m[r];
-        slot[BM * DH + BM + row] = l[r];
+        slot[BM * DH + wave * 32 + r * 16 + l16] = w.m[r];
+        slot[BM * DH + BM + wave * 32 + r * 16 + l16] = l[r];
       }
     }
     return;
@@ -732,8 +728,43 @@ __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(Pa
   for (int i = 0; i < 32 / RPL; ++i) {
     const int row = i * RPL + lane / CPR, chunk = lane % CPR;
     const u32x4 o = *reinterpret_cast<const u32x4*>(smem + own + row * ROWB + (chunk ^ (row % CPR)) * 16);
-    if (wave * 32 + row < at.rows) *reinterpret_cast<u32x4*>(p.out + out_rows[wave * 32 + row] + chunk * 8) = o;
+    if (wave * 32 + row < at.rows) *reinterpret_cast<u32x4*>(p.out + shared.out_rows[wave * 32 + row] + chunk * 8) = o;
   }
+}
+
+// A workgroup per block (and part: more than 256 sequences), the longest first
+template <int DH>
+__global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(PackedDev p) {
+  __shared__ __attribute__((aligned(1024))) ManyShared<DH> shared;
+  const int kvh = blockIdx.x % p.n_kv, unit = blockIdx.x / p.n_kv;
+  const int part = unit % p.max_parts, g = p.rows.n_blocks - 1 - unit / p.max_parts;
+  Place at;
+  if (!find_block<kManyRows>(p.rows, g, at)) return;
+  const int tiles = (row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys, n_parts = parts_of(p, tiles);
+  if (part >= n_parts) return;
+  const int first = (int)((long)tiles * part / n_parts);
+  many_rows<DH>(p, at, kvh, first, (int)((long)tiles * (part + 1) / n_parts) - first,
+                n_parts > 1 ? part_slot<DH, kManyRows>(p, g, kvh, part) : nullptr, shared);
+}
+// Blocks whose keys are cut, by the lengths on the device, into no more parts than there are workgroups
+template <int DH, int S>
+__global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_parts_kernel(PackedDev p) {
+  __shared__ __attribute__((aligned(1024))) ManyShared<DH> shared;
+  const int kvh = blockIdx.x % p.n_kv, u = blockIdx.x / p.n_kv;
+  Layout<kManyRows, kManyKeys, S, true> all;
+  all.read(p.rows, p.n_kv, p.slots, p.max_parts);
+  if (u >= all.n_units) return;
+  Place at;
+  int block, part, n_parts;
+  all.unit(p.rows, u, at, block, part, n_parts);
+  // (offsets that do not ascend can lead anywhere)
+  if (at.row0 < 0 || at.rows <= 0 || (unsigned)block >= (unsigned)p.rows.n_blocks || (unsigned)part >= (unsigned)n_parts) return;
+  const int tiles = (row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys;
+  n_parts = all.needed(tiles, n_parts);
+  if (part >= n_parts) return;
+  const int first = (int)((long)tiles * part / n_parts);
+  many_rows<DH>(p, at, kvh, first, (int)((long)tiles * (part + 1) / n_parts) - first,
+                n_parts > 1 ? part_slot<DH, kManyRows>(p, block, kvh, part) : nullptr, shared);
 }
 
 // ---- parts of a row's keys, joined ---------------------------------------------------------------
@@ -761,8 +792,8 @@ __global__ void __launch_bounds__(256) attn_packed_join_few_kernel(PackedDev p) 
   int n_parts;
   const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
   if constexpr (S > 0) {
-    Layout<BM, kFewKeys, S> all;
-    all.read(p.rows, p.n_kv, kFewSlots, p.max_parts);
+    Layout<BM, kFewKeys, S, false> all;
+    all.read(p.rows, p.n_kv, p.slots, p.max_parts);
     if (g >= all.n_blocks) return;
     all.block(p.rows, g, at, n_parts);
     if (at.row0 < 0) return;
@@ -805,17 +836,28 @@ __global__ void __launch_bounds__(256) attn_packed_join_few_kernel(PackedDev p) 
   if (side == 0) join_store(p, at, row, c, DH, sum, l);
 }
 
-// Many rows, few parts: a thread per row and four channels, four parts at once.
-template <int DH>
+// Many rows, few parts: a thread per row and four channels, as a lane of the parts held them, four parts at once.
+template <int DH, int S>
 __global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p) {
-  constexpr int LANES = DH / 4, AT_ONCE = 4, BM = kManyRows;
+  constexpr int CB = DH / 16, AT_ONCE = 4, BM = kManyRows;
   constexpr long SLOT = packed_slot_floats(DH, BM);
-  const int row = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
-  Place at;
+  const int lane = threadIdx.x & 63, f = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = f / (2 * CB) * 32 + (f & 1) * 16 + (lane & 15), c = (f >> 1) % CB * 16 + (lane >> 4) * 4;
   const int kvh = blockIdx.x % p.n_kv, g = blockIdx.x / p.n_kv;
-  if (!find_block<BM>(p.rows, g, at) || row >= at.rows) return;
-  const int n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys);
-  if (n_parts < 2) return;
+  Place at;
+  int n_parts;
+  if constexpr (S > 0) {
+    Layout<BM, kManyKeys, S, true> all;
+    all.read(p.rows, p.n_kv, p.slots, p.max_parts);
+    if (g >= all.n_blocks) return;
+    all.block(p.rows, g, at, n_parts);
+    if (at.row0 < 0) return;
+    n_parts = all.needed((row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys, n_parts);
+  } else {
+    if (!find_block<BM>(p.rows, g, at)) return;
+    n_parts = parts_of(p, (row_limit(p.rows, at, at.row0 + at.rows - 1) + kManyKeys - 1) / kManyKeys);
+  }
+  if (row >= at.rows || n_parts < 2) return;
   const float* slot = part_slot<DH, BM>(p, g, kvh, 0);
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   float m = -__FLT_MAX__, l = 0.f;
@@ -827,7 +869,7 @@ __global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p)
       const float* from = slot + (q0 + i < n_parts ? q0 + i : n_parts - 1) * SLOT;
       mq[i] = from[BM * DH + row];
       lq[i] = from[BM * DH + BM + row];
-      v[i] = *reinterpret_cast<const f32x4*>(from + row * DH + c);
+      v[i] = reinterpret_cast<const f32x4*>(from)[f * 64 + lane];
     }
     __builtin_amdgcn_sched_barrier(0);
     float m_new = m;
@@ -850,7 +892,7 @@ __global__ void __launch_bounds__(256) attn_packed_join_many_kernel(PackedDev p)
 template <int DH, int R, int S>
 hipError_t launch_few_laid(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
   const long most = (long)plan.blocks * plan.parts * p.n_kv;
-  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R, S>), dim3((unsigned)(most < kFewSlots ? most : kFewSlots)), dim3(kFewWaves<DH> * 64), 0, s, p);
+  hipLaunchKernelGGL((attn_packed_few_kernel<DH, R, S>), dim3((unsigned)(most < p.slots ? most : p.slots)), dim3(kFewWaves<DH> * 64), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.parts == 1) return e;
   hipLaunchKernelGGL((attn_packed_join_few_kernel<DH, 16 * R, S>), dim3((unsigned)(plan.blocks * p.n_kv), 4 * R), dim3(256), 0, s, p);
@@ -868,14 +910,21 @@ hipError_t launch_few(const PackedDev& p, const PackedPlan& plan, hipStream_t s)
   return hipGetLastError();
 }
 
-template <int DH>
-hipError_t launch_many(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
-  const dim3 grid((unsigned)((long)plan.blocks * plan.parts * p.n_kv));
-  hipLaunchKernelGGL(attn_packed_many_kernel<DH>, grid, dim3(kManyWaves * 64), 0, s, p);
+template <int DH, int S>
+hipError_t launch_many_cut(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  if (S > 0)
+    hipLaunchKernelGGL((attn_packed_many_parts_kernel<DH, S == 0 ? 1 : S>), dim3((unsigned)p.slots), dim3(kManyWaves * 64), 0, s, p);
+  else
+    hipLaunchKernelGGL(attn_packed_many_kernel<DH>, dim3((unsigned)((long)plan.blocks * plan.parts * p.n_kv)), dim3(kManyWaves * 64), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.parts == 1) return e;
-  hipLaunchKernelGGL(attn_packed_join_many_kernel<DH>, dim3((unsigned)(plan.blocks * p.n_kv), kManyRows * DH / 1024), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((attn_packed_join_many_kernel<DH, S>), dim3((unsigned)(plan.blocks * p.n_kv), kManyRows * DH / 1024), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+template <int DH>
+hipError_t launch_many(const PackedDev& p, const PackedPlan& plan, hipStream_t s) {
+  if (plan.parts == 1 || p.rows.batch > 256) return launch_many_cut<DH, 0>(p, plan, s);
+  return p.rows.batch <= 64 ? launch_many_cut<DH, 1>(p, plan, s) : launch_many_cut<DH, 4>(p, plan, s);
 }
 
 template <int DH>
@@ -912,6 +961,13 @@ hipError_t launch_attn_packed_bf16(const PackedArgs& a, hipStream_t s) {
   p.n_kv = a.n_kv_heads;
   p.max_parts = plan.parts;
   p.part_tiles = plan.part_keys / (plan.rows == kManyRows ? kManyKeys : kFewKeys);
+  // (two on every CU; with many rows, n_kv times a number, and at least two per block that there can be, four where masked rows
+  // see half of the keys on average)
+  p.slots = 512;
+  if (plan.rows == kManyRows) {
+    const long least = (a.causal_block > 0 && 2l * a.max_q > a.max_k ? 4l : 2l) * plan.blocks;
+    p.slots = (int)((512 / a.n_kv_heads > least ? 512 / a.n_kv_heads : least) * a.n_kv_heads);
+  }
   p.parts = a.workspace;
   p.scale_log2 = a.scale * kLog2e;
   return a.head_dim == 128 ? launch_dh<128>(p, plan, s) : launch_dh<64>(p, plan, s);

@@ -84,11 +84,13 @@ __device__ __forceinline__ int wave_prefix_sum(int v) {
 // All sequences of a launch (64 S at most), S in each lane: their blocks of BM rows and the parts that the keys of a block (tiles of
 // KEYS) are cut into, by the lengths as they are and not as the host knows them, without a number for a block or a part that is not there.
 // Blocks are numbered by lane, then by sequence of the lane.
-template <int BM, int KEYS, int S>
+// FIT: no more parts than slots, which are at least twice the blocks.
+template <int BM, int KEYS, int S, bool FIT>
 struct Layout {
   int q0[S], len_q[S], k0[S], len_k[S], blocks[S], parts[S];
   int blocks_upto, units_upto;  // of the lanes up to and including this one
   int n_blocks, n_units;        // in all
+  int part_tiles;
 
   // slots: workgroups that run at once.  A part is what makes about as many parts as there are slots (with many blocks, four for every
   // block), each block's last one half full; 4 tiles at least.
@@ -120,10 +122,11 @@ struct Layout {
     }
     blocks_upto = wave_prefix_sum(own_blocks);
     n_blocks = __builtin_amdgcn_readlane(blocks_upto, 63);
-    int part_tiles = 1 << 30;
+    part_tiles = 1 << 30;
     if (max_parts > 1) {
-      const float pairs = (float)n_blocks * (float)n_kv, wanted = pairs <= 0.5f * (float)slots ? (float)slots : 4.f * pairs;
-      part_tiles = (int)(wave_sum(work) * (float)n_kv / (wanted - 0.5f * pairs)) + 1;
+      // (cut into parts of P tiles, n blocks make less than their tiles / P + n parts)
+      const float pairs = (float)n_blocks * (float)n_kv, wanted = FIT || pairs <= 0.5f * (float)slots ? (float)slots : 4.f * pairs;
+      part_tiles = (int)(wave_sum(work) * (float)n_kv / (wanted - (FIT ? 1.f : 0.5f) * pairs)) + 1;
       part_tiles = __builtin_amdgcn_readfirstlane(part_tiles < 4 ? 4 : part_tiles);
     }
     int own_units = 0;
@@ -138,6 +141,11 @@ struct Layout {
     n_units = __builtin_amdgcn_readlane(units_upto, 63);
   }
 
+  // Parts of a block that sees `tiles` only, of the n_parts that its sequence's keys would make
+  __device__ __forceinline__ int needed(int tiles, int n_parts) const {
+    const int n = (int)((unsigned)(tiles + part_tiles - 1) / (unsigned)part_tiles);
+    return n < 1 ? 1 : n < n_parts ? n : n_parts;
+  }
   // Place of block `local` of sequence i of lane l
   __device__ __forceinline__ void place(const PackedRows& p, int l, int i, int local, Place& at, int& n_parts) const {
 #pragma unroll
