@@ -184,8 +184,8 @@ dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, in
  *   rows   NULL: k_out and v_out have a row per token.  Else [n_tokens] int32: token t goes to row rows[t] of them, nowhere if that is
  *          outside [0, out_rows); no two tokens to the same row
  * Each of q, k and v may be NULL (with its output).  q_out may be q, and without rows k_out k and v_out v (with the same
- * ld); there is no other overlap.  head_dim is a multiple of 8 up to 256, rot_dim even, 2 .. head_dim.  Alignment that is less than 16
- * bytes, and halves of which no 16 bytes have their partners in 16, are taken element by element.
+ * ld); there is no other overlap.  head_dim is a multiple of 8 up to 256, rot_dim even, 2 .. head_dim.  Rows need no
+ * alignment but that of their elements.
  */
 enum { DARE_ROPE_HALF = 0, DARE_ROPE_PAIRS = 1 };
 dare_status dare_k_rope(int dtype, int layout, int n_tokens, int head_dim, int rot_dim, const int32_t* pos,

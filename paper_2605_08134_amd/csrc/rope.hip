@@ -11,7 +11,9 @@
 // What bounds it: bytes where there are many tokens, latencies where there are few.  So a lane asks for its first kAtOnce items
 // before it turns to the angles, and few tokens are spread over as many waves as they have items for (rope_split).  us, 32 and 8 heads of
 // 128 channels, bf16, part by part with the angles first and now: 1 token 4.4 and 2.9, 8 4.8 and 3.0, 300 7.5 and 3.8,
-// 16384 81.2 and 82.8 (4.9 TB/s; a large copy reaches 5.0); 2, 4 and 8 items at once 82.8, 84.2, 83.1.
+// 16384 81.2 and 82.8 (4.9 TB/s; a large copy reaches 5.0); 2, 4 and 8 items at once 82.8, 84.2, 83.1.  Halves that no
+// 16 bytes divide: 9161 tokens of 16 and 4 heads, 34 of 128 channels rotated, element by element 87 us, in chunks and what they leave 53 (chunks of
+// 16 bytes each, 48 channels, 34).
 #include "dare_common.h"
 #include "attn_packed.h"
 
@@ -36,17 +38,20 @@ struct RopeDev {
 
 constexpr int kRopeWaves = 4, kAtOnce = 2;
 
-// V elements (of type E) that are read and written at once
-template <class E, int V>
-struct alignas(V * sizeof(E) == 16 ? 16 : sizeof(E)) Chunk {
+// 16 bytes, V elements of type E, that are read and written at once, also where they do not lie on 16 bytes (ALIGNED)
+template <class E, bool ALIGNED>
+struct alignas(ALIGNED ? 16 : sizeof(E)) Chunk {
+  static constexpr int V = 16 / sizeof(E);
   E v[V];
 };
 
 // PAIRS: channels (2 i, 2 i + 1) are a pair, an item is a chunk of V neighbouring channels.  Else i and i + rot / 2: an item is a chunk
-// of V channels i with the one of their partners, or a chunk of channels that are not rotated.
-template <class E, int V, bool PAIRS>
+// of V channels i with the one of their partners, or a chunk of channels that are not rotated; !WHOLE: or one channel, with its partner
+// or without, of those that are left over where rot / 2 is not a multiple of V.
+template <class E, bool PAIRS, bool ALIGNED, bool WHOLE>
 __global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
-  typedef Chunk<E, V> chunk_t;
+  typedef Chunk<E, ALIGNED> chunk_t;
+  constexpr int V = chunk_t::V;
   __shared__ float cs_all[kRopeWaves][kRopeMaxDim];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long t = (long)blockIdx.x * kRopeWaves + wave;
@@ -61,6 +66,7 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
     E* base[kAtOnce];   // the part's output row (the same in all lanes)
     int at[kAtOnce];    // the item's first channel in it, -1: no item
     int pair[kAtOnce];  // number of the item's first pair, -1 if none of its channels is rotated
+    bool one[kAtOnce];  // the item is one channel (and its partner)
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const int w = w0 + i * step;
@@ -74,16 +80,29 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
       const int head = divide(item, p.by_per_head[part]), u = item - head * p.per_head[part];
       int c = u * V;      // first channel
       bool turns = part < 2 && c < p.rot;
+      one[i] = false;
       if (!PAIRS && part < 2) {
-        turns = c < half;
-        c += turns ? 0 : half;
+        if (WHOLE) {
+          turns = c < half;
+          c += turns ? 0 : half;
+        } else {
+          const int chunks = half / V, turning = chunks + half % V, rest = p.dim - p.rot;
+          turns = u < turning;
+          const int k = turns ? u : u - turning;
+          one[i] = turns ? k >= chunks : rest < V;
+          c = one[i] ? (turns ? chunks * V + k - chunks : p.rot + k) : (turns ? 0 : p.rot) + k * V;
+          c = turns || one[i] || c + V <= p.dim ? c : p.dim - V;  // (the last chunk that is not rotated may overlap the one before)
+        }
       }
       at[i] = head * p.dim + c;
-      a[i] = *reinterpret_cast<const chunk_t*>(src + at[i]);
-      if (turns) {
-        pair[i] = PAIRS ? c >> 1 : c;
-        if (!PAIRS) b[i] = *reinterpret_cast<const chunk_t*>(src + at[i] + half);
+      if (turns) pair[i] = PAIRS ? c >> 1 : c;
+      if (!WHOLE && one[i]) {
+        a[i].v[0] = src[at[i]];
+        if (turns) b[i].v[0] = src[at[i] + half];
+        continue;
       }
+      a[i] = *reinterpret_cast<const chunk_t*>(src + at[i]);
+      if (turns && !PAIRS) b[i] = *reinterpret_cast<const chunk_t*>(src + at[i] + half);
     }
     if (w0 == (int)blockIdx.y) {
       __builtin_amdgcn_sched_barrier(0);
@@ -104,10 +123,11 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       if (at[i] < 0) continue;
+      E* const to = base[i] + at[i];
       if (PAIRS) {
-        if (V > 1 && pair[i] >= 0) {
+        if (pair[i] >= 0) {
 #pragma unroll
-          for (int e = 0; e + 1 < V; e += 2) {
+          for (int e = 0; e < V; e += 2) {
             const int j = pair[i] + (e >> 1);
             if (j < half) {
               const float x = (float)a[i].v[e], y = (float)a[i].v[e + 1], co = cs[2 * j], si = cs[2 * j + 1];
@@ -119,14 +139,21 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_kernel(RopeDev p) {
       } else if (pair[i] >= 0) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
+          if (!WHOLE && one[i] && e > 0) break;
           const float co = cs[2 * (pair[i] + e)], si = cs[2 * (pair[i] + e) + 1];
           const float x = (float)a[i].v[e], y = (float)b[i].v[e];
           a[i].v[e] = (E)(x * co - y * si);
           b[i].v[e] = (E)(y * co + x * si);
         }
-        *reinterpret_cast<chunk_t*>(base[i] + at[i] + half) = b[i];
+        if (!WHOLE && one[i])
+          to[half] = b[i].v[0];
+        else
+          *reinterpret_cast<chunk_t*>(to + half) = b[i];
       }
-      *reinterpret_cast<chunk_t*>(base[i] + at[i]) = a[i];
+      if (!WHOLE && one[i])
+        to[0] = a[i].v[0];
+      else
+        *reinterpret_cast<chunk_t*>(to) = a[i];
     }
   }
 }
@@ -137,21 +164,24 @@ int rope_split(int n, int turns) {
   return want < turns ? want : turns;
 }
 
-// V: elements at once where that is possible; NARROW: channel by channel, or pair by pair where they are neighbours
-template <class E, int V, bool NARROW>
-hipError_t launch_layout(RopeDev p, const int (&heads)[3], bool pairs, hipStream_t s) {
-  const int v = !NARROW ? V : pairs ? 2 : 1;
+template <class E>
+hipError_t launch_layout(RopeDev p, const int (&heads)[3], bool pairs, bool aligned, hipStream_t s) {
+  constexpr int V = 16 / sizeof(E);
+  const int half = p.rot / 2, rest = p.dim - p.rot;
   for (int i = 0, end = 0; i < 3; ++i) {
-    p.per_head[i] = !pairs && i < 2 ? p.rot / 2 / v + (p.dim - p.rot) / v : p.dim / v;
+    p.per_head[i] = pairs || i == 2 ? p.dim / V : half / V + half % V + (rest < V ? rest : (rest + V - 1) / V);
     p.by_per_head[i] = divider(p.per_head[i]);
     p.items[i] = heads[i] * p.per_head[i];
     p.turns[i] = end += (p.items[i] + 63) / 64;
   }
   const dim3 grid((p.n + kRopeWaves - 1) / kRopeWaves, rope_split(p.n, p.turns[2])), block(kRopeWaves * 64);
-  if (pairs)
-    hipLaunchKernelGGL((rope_kernel<E, NARROW ? 2 : V, true>), grid, block, 0, s, p);
-  else
-    hipLaunchKernelGGL((rope_kernel<E, NARROW ? 1 : V, false>), grid, block, 0, s, p);
+  if (pairs) {
+    if (aligned) hipLaunchKernelGGL((rope_kernel<E, true, true, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((rope_kernel<E, true, false, true>), grid, block, 0, s, p);
+  } else {
+    if (aligned && half % V == 0) hipLaunchKernelGGL((rope_kernel<E, false, true, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((rope_kernel<E, false, false, false>), grid, block, 0, s, p);
+  }
   return hipGetLastError();
 }
 
@@ -161,7 +191,7 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
   RopeDev p{};
   const size_t esize = dtype == DARE_BF16 ? 2 : 4;
-  uintptr_t bits = 0;  // of everything that has to be a multiple of 16 bytes
+  uintptr_t bits = 0;  // of all that lies on 16 bytes or does not
   int heads[3];
   for (int i = 0; i < 3; ++i) {
     p.x[i] = a.x[i];
@@ -179,12 +209,8 @@ hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s) {
   p.rows = a.rows;
   p.out_rows = a.out_rows;
   p.magnitude = a.magnitude;
-  // 16 bytes at a time where everything lies on such a boundary and, by halves, a chunk has its partners in one chunk
-  const int v = (int)(16 / esize);
-  const bool wide = bits % 16 == 0 && a.dim % v == 0 && (a.pairs || (a.rot / 2) % v == 0);
-  if (dtype == DARE_BF16)
-    return wide ? launch_layout<bf16_t, 8, false>(p, heads, a.pairs, s) : launch_layout<bf16_t, 8, true>(p, heads, a.pairs, s);
-  return wide ? launch_layout<float, 4, false>(p, heads, a.pairs, s) : launch_layout<float, 4, true>(p, heads, a.pairs, s);
+  return dtype == DARE_BF16 ? launch_layout<bf16_t>(p, heads, a.pairs, bits % 16 == 0, s)
+                            : launch_layout<float>(p, heads, a.pairs, bits % 16 == 0, s);
 }
 
 }  // namespace dare
