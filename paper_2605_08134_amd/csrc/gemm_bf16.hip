@@ -1520,6 +1520,15 @@ __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsig
 #pragma unroll
       for (int u = 0; u < UNR; ++u) {
         const bool live = s + u < s1;
+        if (LINEAR && !live) {  // (nothing is loaded, and no infinity meets a zero)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            wf[u][e] = (bf16_t)0.0f;
+#pragma unroll
+            for (int t = 0; t < TMS; ++t) xf[t][u][e] = (bf16_t)0.0f;
+          }
+          continue;
+        }
         const int ks = (live ? s + u : s0) << 5;
         wf[u] = *reinterpret_cast<const bf16x8*>(wrow + ks);
 #pragma unroll
@@ -1527,12 +1536,6 @@ __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsig
         if (!live) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) wf[u][e] = (bf16_t)0.0f;
-          if constexpr (LINEAR) {  // (0 times an infinity is none)
-#pragma unroll
-            for (int t = 0; t < TMS; ++t)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) xf[t][u][e] = (bf16_t)0.0f;
-          }
         }
       }
 #pragma unroll
@@ -1590,7 +1593,7 @@ __global__ void __launch_bounds__(512) gemm_bf16_pp_kernel(GemmDev p) {
 
 // ---- act(A W + bias) + residual of all rows ---------------------------------------------------
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
-__global__ void __launch_bounds__(512) linear_bf16_tile16_kernel(GemmDev p) {
+__global__ void __launch_bounds__(WAVES_M* WAVES_N * 64) linear_bf16_tile16_kernel(GemmDev p) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[smem_bytes<BM, BN, STAGES>()];
   gemm_tile16<BM, BN, WAVES_M, WAVES_N, STAGES, true>(p, p.m_max, smem, threadIdx.x, blockIdx.x);
 }
@@ -1604,10 +1607,9 @@ __global__ void __launch_bounds__(256, 1) linear_bf16_quad_kernel(GemmDev p) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kQuadSmem];
   gemm_tiles_quad<TN, STREAM, false, true>(p, p.m_max, smem);
 }
-template <int TMS>
 __global__ void __launch_bounds__(512) linear_bf16_skinny_kernel(GemmDev p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[8 * TMS * 64 * 16];
-  skinny_tile<8, TMS, true>(p, p.m_max, smem, threadIdx.x);
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[8 * 64 * 16];
+  skinny_tile<8, 1, true>(p, p.m_max, smem, threadIdx.x);
 }
 
 // ---- row count read on the device: the tile shape follows it -------------------------
@@ -2156,11 +2158,17 @@ hipError_t launch_rows_wide(const GemmArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The shapes of the plain projection by its rule, and the stream over the weights for few rows of narrow outputs
+// The shapes of the plain projection by its rule, but for few rows, where the CUs that have a tile pull the operands:
+//   * up to 8 rows of narrow outputs: the stream over the weights, one workgroup per 16 columns.  It pulls every row once per 16
+//     columns and in pieces of 64 bytes, so with more rows tiles are faster: n x k = 4096 x 4096, 4096 x 12288, 2176 x 9408, 448 x 4352, 8 rows 9.3
+//     28.9 16.8 8.1 us, 16 rows 10.6 34.1 19.7 10.0, 32 rows 14.4 45.0 29.7 18.4;
+//   * up to 32 rows of narrow outputs: 32 x 32 in eight stages (16 rows 9.6 32.7 17.0 9.0, 32 rows 9.7 36.1 17.2 9.1, with sixteen
+//     stages 10.4 36.8 17.8 9.5; 32 x 64 13.2 52.1 23.9 12.4);
+//   * as long as 64 x 64 leave half of the CUs without a tile: 64 x 32 (64 rows, 64 x 64 and this, 14.9 13.4, 63.3 49.0, 28.3 24.1).
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 hipError_t launch_linear_tile16(const GemmArgs& g, hipStream_t s) {
   hipLaunchKernelGGL((linear_bf16_tile16_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>),
-                     dim3(grid_for(tiles_of(g.m_max, g.n, BM, BN))), dim3(512), 0, s, to_dev(g));
+                     dim3(grid_for(tiles_of(g.m_max, g.n, BM, BN))), dim3(WAVES_M * WAVES_N * 64), 0, s, to_dev(g));
   return hipGetLastError();
 }
 template <int TN>
@@ -2180,13 +2188,12 @@ hipError_t launch_linear_quad(const GemmArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_linear(const GemmArgs& g, hipStream_t s) {
-  if (g.m_max <= kSkinnyRows && g.n < kSkinnyMaxN) {
-    if (g.m_max <= 16)
-      hipLaunchKernelGGL(linear_bf16_skinny_kernel<1>, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
-    else
-      hipLaunchKernelGGL(linear_bf16_skinny_kernel<2>, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
+  if (g.m_max <= 8 && g.n < kSkinnyMaxN) {
+    hipLaunchKernelGGL(linear_bf16_skinny_kernel, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
     return hipGetLastError();
   }
+  if (g.m_max <= 32 && g.n < kSkinnyMaxN) return launch_linear_tile16<32, 32, 2, 2, 8>(g, s);
+  if (tiles_of(g.m_max, g.n, 64, 64) <= 128) return launch_linear_tile16<64, 32, 4, 2, 6>(g, s);
   switch (gemm_route(g.m_max, g.n, g.k, 1, false)) {
     case GemmRoute::kQuad256: return launch_linear_quad<4>(g, s);
     case GemmRoute::kQuad192: return launch_linear_quad<3>(g, s);
