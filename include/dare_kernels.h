@@ -225,8 +225,8 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
  * workspace: dare_k_attention_packed_workspace() bytes (for the same config), 16-byte aligned, needed while the call runs, not
  * initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, n_heads not a multiple of n_kv_heads, scale not above 0 or not
- * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; total_q * n_heads + 128 batch, or the grid, beyond
- * 2^31).
+ * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; total_q * n_heads + 128 batch, or
+ * batch * n_kv_heads, beyond 2^31).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_packed_config) */

@@ -65,6 +65,9 @@ constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, i
   long parts = max_k / (plan.rows < 128 || even > 512 ? 512 : even > 256 ? even : 256);
   if (plan.rows < 128 && batch <= 256 && parts > 0) parts = max_k / 128;
   if (parts > room) parts = room;
+  // (a slot of the workspace for every part of every block that there can be: 270 MB at most)
+  const long slots = (plan.rows == 128 ? 4096 : 16384) / ((long)plan.blocks * n_kv + 1);
+  if (parts > slots) parts = slots;
   if (parts > kPackedMaxParts) parts = kPackedMaxParts;
   if (parts > 1) {
     plan.parts = (int)parts;

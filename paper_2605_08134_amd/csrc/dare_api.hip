@@ -1200,6 +1200,8 @@ dare_status check_packed(const dare_packed_config* c, PackedArgs* a) {
   if (c->ldq < wq || c->ldo < wq || c->ldk < wk || c->ldv < wk) return refuse("ld below the width of a row");
   if (c->ldq > kMaxLd || c->ldo > kMaxLd || c->ldk > kMaxLd || c->ldv > kMaxLd) return unsupported("ld beyond 2^24");
   if ((long)c->total_q * c->n_heads + 128l * c->batch >= 1l << 31) return unsupported("more than 2^31 query rows");
+  if (((long)c->total_q * (c->n_heads / c->n_kv_heads) / 16 + c->batch) * c->n_kv_heads >= 1l << 31)
+    return unsupported("more than 2^31 blocks of rows");
   a->ldq = c->ldq;
   a->ldk = c->ldk;
   a->ldv = c->ldv;

@@ -262,7 +262,8 @@ def test_attention_of_prompts(dtype, d, lens, block, h, kv, pad):
     assert ou.worst(out, want, bound) <= 1.0
 
 
-@pytest.mark.parametrize("h,kv,d,lq,lk", [(8, 1, 128, 1, 5000), (4, 1, 64, 3, 9001), (16, 4, 128, 16, 2500), (8, 2, 128, 32, 4100)])
+@pytest.mark.parametrize("h,kv,d,lq,lk", [(8, 1, 128, 1, 5000), (4, 1, 64, 3, 9001), (16, 4, 128, 16, 2500), (8, 2, 128, 32, 4100),
+                                            (8, 2, 64, 7, 3000), (14, 2, 128, 4, 2600), (6, 2, 64, 50, 2300)])
 @pytest.mark.parametrize("block", [0, 1])
 def test_attention_over_a_long_cache(h, kv, d, lq, lk, block):
     """Keys of a row cut over workgroups."""
@@ -291,6 +292,38 @@ def test_attention_of_many_sequences(batch):
     for h, kv, d, dtype in ((4, 2, 64, "bf16"), (2, 2, 64, "f32")):
         q, k, v = ou.rand(g, off[-1], h, d, dtype=dtype), ou.rand(g, kb[-1], kv, d, dtype=dtype), ou.rand(g, kb[-1], kv, d, dtype=dtype)
         _check_attention(q, k, v, off, kb[:-1], kb[1:], 1)
+
+
+@pytest.mark.parametrize("batch", [70, 300])
+@pytest.mark.parametrize("h,kv,d,q_most,k_most", [(4, 1, 64, 1, 3000), (4, 1, 128, 40, 1500), (2, 2, 64, 90, 90)])
+def test_attention_of_many_sequences_of_many_lengths(batch, h, kv, d, q_most, k_most):
+    """More than 64, and more than 256, sequences, a few of them long: keys cut with both ways of finding a block."""
+    g = _gen(batch + q_most)
+    lq = torch.randint(0, 3, (batch,), generator=g).clamp(max=q_most).tolist()
+    lk = [n + int(x) for n, x in zip(lq, torch.randint(0, 9, (batch,), generator=g))]
+    for i in (1, batch // 2, batch - 1):
+        lq[i], lk[i] = q_most, k_most
+    off, kb = _offsets(lq), _offsets(lk)
+    q, k, v = ou.rand(g, off[-1], h, d, dtype="bf16"), ou.rand(g, kb[-1], kv, d, dtype="bf16"), ou.rand(g, kb[-1], kv, d, dtype="bf16")
+    cut = B.dare_k_attention_packed_workspace(B.DARE_BF16, batch, off[-1], q_most, k_most, h, kv, d) > 0
+    assert cut == (k_most > 1000)
+    for block in (0, 1):
+        _check_attention(q, k, v, off, kb[:-1], kb[1:], block)
+
+
+@pytest.mark.parametrize("q_off,most", [([0, 6, 2, 8, 3], 1), ([0, 8, 0, 8, 0], 6), ([5, 3, 1, 0, 0], 1), ([0, 2 ** 31 - 1, -5, 9, 4], 40)])
+@pytest.mark.parametrize("batch", [4, 80])
+def test_attention_with_offsets_that_do_not_ascend_stays_inside(q_off, most, batch):
+    """Whatever they lead to, rows that no sequence can have are left alone, and the call ends."""
+    g = _gen(most)
+    q_off = q_off + [q_off[-1]] * (batch - 4)
+    for h, kv, d, dtype in ((4, 1, 64, "bf16"), (4, 1, 128, "bf16"), (2, 1, 64, "f32")):
+        q, k, v = (ou.rand(g, n, x, d, dtype=dtype).cuda() for n, x in ((8, h), (1500, kv), (1500, kv)))
+        buf = torch.full((24, h, d), 7.0, dtype=q.dtype, device="cuda")
+        _run_attention(q, k, v, q_off, [0, 700, 3, 9] * (batch // 4), [1500, 1400, 1100, 1200] * (batch // 4), 1, out=buf[8:16],
+                       max_q=most, max_k=1500)
+        torch.cuda.synchronize()
+        assert (buf[:8] == 7).all() and (buf[16:] == 7).all() and torch.isfinite(buf).all()
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])

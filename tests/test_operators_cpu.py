@@ -92,6 +92,7 @@ def _packed(**kw):
     (dict(head_dim=96), B.DARE_ERR_UNSUPPORTED), (dict(ldq=248), B.DARE_ERR_INVALID_ARG), (dict(ldk=120), B.DARE_ERR_INVALID_ARG),
     (dict(ldo=1 << 25), B.DARE_ERR_UNSUPPORTED), (dict(total_q=2 ** 31 - 1), B.DARE_ERR_UNSUPPORTED),
     (dict(batch=2 ** 24), B.DARE_ERR_UNSUPPORTED),
+    (dict(batch=2 ** 23, n_heads=256, n_kv_heads=256, ldq=2 ** 14, ldk=2 ** 14, ldv=2 ** 14, ldo=2 ** 14), B.DARE_ERR_UNSUPPORTED),
 ])
 def test_attention_refuses_a_config(L, kw, want):
     cfg, need = _packed(**kw), ctypes.c_size_t(7)
@@ -133,6 +134,15 @@ def test_binding_refuses_what_is_not_on_the_gpu():
         B.dare_k_rope(i, torch.zeros(32, dtype=torch.float64), "half")
     with pytest.raises(ValueError):
         B.dare_k_attention_packed(x, x, x, x, i, i, i, 1, 1)
+
+
+def test_the_workspace_stays_small_whatever_the_batch():
+    for batch, total, max_q in ((1, 1, 1), (1 << 20, 1, 1), (300, 300, 1), (64, 64, 1), (64, 2048, 32), (4096, 9000, 700), (16, 512, 32)):
+        for kv in (1, 8, 64):
+            for max_k in (1, 511, 4096, 1 << 20):
+                need = B.dare_k_attention_packed_workspace(B.DARE_BF16, batch, total, max_q, max_k, 4 * kv, kv, 128)
+                assert 0 <= need <= 300 << 20, (batch, total, kv, max_k, need)
+                assert B.dare_k_attention_packed_workspace(B.DARE_F32, batch, total, max_q, max_k, 4 * kv, kv, 128) == 0
 
 
 # ---- the rule ------------------------------------------------------------------------------------
