@@ -188,10 +188,20 @@ dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, in
  * alignment but that of their elements.
  */
 enum { DARE_ROPE_HALF = 0, DARE_ROPE_PAIRS = 1 };
-dare_status dare_k_rope(int dtype, int layout, int n_tokens, int head_dim, int rot_dim, const int32_t* pos,
-                        const double* freqs, float magnitude, const void* q, long ldq, void* q_out, long ldqo, int n_heads,
-                        const void* k, long ldk, void* k_out, long ldko, const void* v, long ldv, void* v_out, long ldvo,
-                        int n_kv_heads, const int32_t* rows, int out_rows, void* hip_stream);
+typedef struct {
+  uint32_t struct_size; /* = sizeof(dare_rope_call) */
+  int32_t dtype, layout, n_tokens, head_dim, rot_dim;
+  int32_t n_heads, n_kv_heads;
+  int32_t out_rows;
+  float magnitude;
+  const int32_t* pos;
+  const double* freqs;
+  const int32_t* rows;
+  const void *q, *k, *v;
+  void *q_out, *k_out, *v_out;
+  int64_t ldq, ldk, ldv, ldqo, ldko, ldvo;
+} dare_rope_call;
+dare_status dare_k_rope(const dare_rope_call* call, void* hip_stream);
 
 /*
  * Frequencies for dare_k_rope: f_i = base^(-2i / rot_dim), changed for contexts longer than the trained one by `factor`:
@@ -222,24 +232,25 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
  *                outside of q, k and v is read, and nothing outside of out written.)
  * max_q and max_k, the largest numbers of query tokens and keys of a sequence, choose how the work is cut: a
  * captured call may be replayed with other lengths.  Longer sequences than they say are right as well, only slower.
- * workspace: dare_k_attention_packed_workspace() bytes (for the same config), 16-byte aligned, needed while the call runs, not
+ * workspace: dare_k_attention_packed_workspace() bytes (for the same call; it does not look at the pointers), 16-byte aligned, needed while the call runs, not
  * initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, n_heads not a multiple of n_kv_heads, scale not above 0 or not
  * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; total_q * n_heads + 128 batch, or
  * batch * n_kv_heads, beyond 2^31).
  */
 typedef struct {
-  uint32_t struct_size; /* = sizeof(dare_packed_config) */
+  uint32_t struct_size; /* = sizeof(dare_packed_call) */
   int32_t dtype, batch, total_q, k_rows, max_q, max_k;
   int32_t n_heads, n_kv_heads, head_dim;
   int32_t causal_block;
   float scale;
   int64_t ldq, ldk, ldv, ldo;
-} dare_packed_config;
-dare_status dare_k_attention_packed_workspace(const dare_packed_config* cfg, size_t* bytes);
-dare_status dare_k_attention_packed(const dare_packed_config* cfg, const void* q, const void* k, const void* v, void* out,
-                                    const int32_t* q_off, const int32_t* k_begin, const int32_t* k_end, void* workspace,
-                                    size_t workspace_bytes, void* hip_stream);
+  const void *q, *k, *v;
+  void* out;
+  const int32_t *q_off, *k_begin, *k_end;
+} dare_packed_call;
+dare_status dare_k_attention_packed_workspace(const dare_packed_call* call, size_t* bytes);
+dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG_DIR, "libdare.so")
@@ -75,18 +76,6 @@ class DareModelConfig(ctypes.Structure):
         ("rope_base", ctypes.c_float),
         ("device", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
-    ]
-
-
-class DarePackedConfig(ctypes.Structure):
-    _fields_ = [
-        ("struct_size", ctypes.c_uint32),
-        ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("total_q", ctypes.c_int32), ("k_rows", ctypes.c_int32),
-        ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
-        ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-        ("causal_block", ctypes.c_int32),
-        ("scale", ctypes.c_float),
-        ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64),
     ]
 
 
@@ -189,14 +178,13 @@ def lib():
     lng = ctypes.c_long
     L.dare_k_linear.argtypes = [i32, vp, lng, vp, i32, i32, i32, vp, i32, vp, lng, vp, lng, vp]
     L.dare_k_linear.restype = i32
-    L.dare_k_rope.argtypes = ([i32] * 5 + [vp, vp, f32] + [vp, lng, vp, lng, i32] + [vp, lng, vp, lng] * 2 + [i32] +
-                              [vp, i32, vp])
+    L.dare_k_rope.argtypes = [vp, vp]
     L.dare_k_rope.restype = i32
     L.dare_k_rope_freqs.argtypes = [vp, i32, ctypes.c_double, i32] + [ctypes.c_double] * 4
     L.dare_k_rope_freqs.restype = i32
-    L.dare_k_attention_packed.argtypes = [ctypes.POINTER(DarePackedConfig)] + [vp] * 8 + [ctypes.c_size_t, vp]
+    L.dare_k_attention_packed.argtypes = [vp, vp, ctypes.c_size_t, vp]
     L.dare_k_attention_packed.restype = i32
-    L.dare_k_attention_packed_workspace.argtypes = [ctypes.POINTER(DarePackedConfig), ctypes.POINTER(ctypes.c_size_t)]
+    L.dare_k_attention_packed_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
     L.dare_k_attention_packed_workspace.restype = i32
     _lib = L
     return L
@@ -541,7 +529,23 @@ def dare_k_copy_rows(src, dst, idx=None, m_dev=None, stream=None):
 
 
 # ---- decoder layers with shared key heads ------------------------------------------------
-# (A call takes the host about as long as a small kernel the GPU, so every property of a tensor is asked for once.)
+# (A call takes the host about as long as a small kernel the GPU, so every property of a tensor is asked for once, and what
+# has many arguments goes over as the bytes of its struct.)
+
+# dare_rope_call: struct_size, dtype, layout, n_tokens, head_dim, rot_dim, n_heads, n_kv_heads, out_rows, magnitude; pos, freqs,
+# rows; q, k, v; q_out, k_out, v_out; ldq, ldk, ldv, ldqo, ldko, ldvo
+_ROPE_CALL = struct.Struct("@I8ifPPP3P3P6q")
+# dare_packed_call: struct_size, dtype, batch, total_q, k_rows, max_q, max_k, n_heads, n_kv_heads, head_dim, causal_block,
+# scale; ldq, ldk, ldv, ldo; q, k, v, out, q_off, k_begin, k_end
+_PACKED_CALL = struct.Struct("@I10if4q7P")
+
+
+def _pack(layout, *fields):
+    try:
+        return layout.pack(layout.size, *fields)
+    except struct.error as e:
+        raise ValueError("an argument does not fit its type: %s" % e) from None
+
 
 def _gpu_of(like):
     """Device index and dtype code of the tensor that the others have to match."""
@@ -561,19 +565,15 @@ def _wrong(name, t, dt, device, wanted):
                                                                        t.device))
 
 
-def _heads(name, t, dt, device, n, heads, head_dim):
-    """Pointer and row distance of a [n, heads, head_dim] tensor (None: any) whose heads lie one behind the other."""
-    shape = t.shape
-    if len(shape) != 3 or t.dtype is not dt or t.get_device() != device:
-        _wrong(name, t, dt, device, "[tokens, heads, head_dim]")
-    rows, h, d = shape
-    if rows != n and n is not None or h != heads and heads is not None or d != head_dim:
-        _wrong(name, t, dt, device, "[%s, %s, %s]" % (n, heads, head_dim))
+def _ld(name, t, shape, dt, device):
+    """Row distance of a [tokens, heads, head_dim] tensor of that shape whose heads lie one behind the other."""
+    if t.shape != shape or t.dtype is not dt or t.get_device() != device:
+        _wrong(name, t, dt, device, list(shape))
     ld, between, inside = t.stride()
-    if inside != 1 and d > 1 or between != d and h > 1:
-        if t.numel():
-            raise ValueError("the heads of a row of %s must lie one behind the other" % name)
-    return t.data_ptr(), ld if rows > 1 else h * d
+    rows, h, d = shape
+    if (inside != 1 and d > 1 or between != d and h > 1) and rows * h * d:
+        raise ValueError("the heads of a row of %s must lie one behind the other" % name)
+    return ld if rows > 1 else h * d
 
 
 def _matrix(name, t, dt, device, rows, cols):
@@ -645,27 +645,39 @@ def dare_k_rope(pos, freqs, layout="half", q=None, q_out=None, k=None, k_out=Non
     first = q if q is not None else k if k is not None else v
     if first is None or first.dim() != 3 or layout not in ROPE_LAYOUTS:
         raise ValueError("q, k or v must be [tokens, heads, head_dim], layout one of %s" % list(ROPE_LAYOUTS))
-    device, dt, code = _gpu_of(first)
-    n, h, d = first.shape
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
         raise ValueError("an input and its output go together")
-    if q is None:
-        args = [None, 0, None, 0, 0]
-    else:
-        args = [*_heads("q", q, dt, device, n, h, d), *_heads("q_out", q_out, dt, device, n, h, d), h]
-    kv, out_rows, n_out = None, 0, n if rows is None else None
-    for name, x, out in (("k", k, k_out), ("v", v, v_out)):
-        if x is None:
-            args += [None, 0, None, 0]
-            continue
-        args += _heads(name, x, dt, device, n, kv, d)
-        kv = x.shape[1]
-        args += _heads(name + "_out", out, dt, device, n_out, kv, d)
-        n_out = out_rows = out.shape[0]
+    device, dt, code = _gpu_of(first)
+    shape = first.shape
+    n, h, d = shape
+    pq = pqo = pk = pko = pv = pvo = None
+    ldq = ldqo = ldk = ldko = ldv = ldvo = kv = out_rows = 0
+    if q is not None:
+        pq, ldq = q.data_ptr(), _ld("q", q, shape, dt, device)
+        pqo, ldqo = q_out.data_ptr(), _ld("q_out", q_out, shape, dt, device)
+    if k is not None or v is not None:
+        one, one_out = (k, k_out) if k is not None else (v, v_out)
+        shape = out_shape = one.shape
+        if len(shape) != 3 or shape[0] != n or shape[2] != d:
+            raise ValueError("k and v must be [%d, heads, %d], not %s" % (n, d, tuple(shape)))
+        kv = shape[1]
+        if rows is not None:
+            out_shape = one_out.shape
+            if len(out_shape) != 3 or out_shape[1] != kv or out_shape[2] != d:
+                raise ValueError("k_out and v_out must be [rows, %d, %d], not %s" % (kv, d, tuple(out_shape)))
+            out_rows = out_shape[0]
+        if k is not None:
+            pk, ldk = k.data_ptr(), _ld("k", k, shape, dt, device)
+            pko, ldko = k_out.data_ptr(), _ld("k_out", k_out, out_shape, dt, device)
+        if v is not None:
+            pv, ldv = v.data_ptr(), _ld("v", v, shape, dt, device)
+            pvo, ldvo = v_out.data_ptr(), _ld("v_out", v_out, out_shape, dt, device)
+    pr = 0 if rows is None else _vector("rows", rows, torch.int32, device, n)
     half = freqs.shape[0]
-    _enqueue(device, stream, lib().dare_k_rope, code, ROPE_LAYOUTS[layout], n, d, 2 * half,
-             _vector("pos", pos, torch.int32, device, n), _vector("freqs", freqs, torch.float64, device, half), magnitude, *args,
-             kv or 0, None if rows is None else _vector("rows", rows, torch.int32, device, n), out_rows)
+    call = _pack(_ROPE_CALL, code, ROPE_LAYOUTS[layout], n, d, 2 * half, 0 if q is None else h, kv, out_rows, magnitude,
+                 _vector("pos", pos, torch.int32, device, n), _vector("freqs", freqs, torch.float64, device, half), pr,
+                 pq or 0, pk or 0, pv or 0, pqo or 0, pko or 0, pvo or 0, ldq, ldk, ldv, ldqo, ldko, ldvo)
+    _enqueue(device, stream, lib().dare_k_rope, call)
 
 
 def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, causal_block=0, scale=None,
@@ -677,38 +689,37 @@ def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, c
     use instead of one of the call's own."""
     import torch
     device, dt, code = _gpu_of(q)
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q and k must be [tokens, heads, head_dim]")
-    total, h, d = q.shape
-    rows, kv, _ = k.shape
+    shape, kshape, i32 = q.shape, k.shape, torch.int32
+    if len(shape) != 3 or len(kshape) != 3 or shape[2] != kshape[2]:
+        raise ValueError("q and k must be [tokens, heads, head_dim], not %s and %s" % (tuple(shape), tuple(kshape)))
+    total, h, d = shape
     batch = k_begin.shape[0]
-    pq, ldq = _heads("q", q, dt, device, total, h, d)
-    pk, ldk = _heads("k", k, dt, device, rows, kv, d)
-    pv, ldv = _heads("v", v, dt, device, rows, kv, d)
-    po, ldo = _heads("out", out, dt, device, total, h, d)
-    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), code, batch, total, rows, max_q, max_k, h, kv, d, causal_block,
-                           d ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
-    ref, i32 = ctypes.byref(cfg), torch.int32
-    offsets = (_vector("q_off", q_off, i32, device, batch + 1), _vector("k_begin", k_begin, i32, device, batch),
-               _vector("k_end", k_end, i32, device, batch))
+    call = _pack(_PACKED_CALL, code, batch, total, kshape[0], max_q, max_k, h, kshape[1], d, causal_block,
+                 d ** -0.5 if scale is None else scale,
+                 _ld("q", q, shape, dt, device), _ld("k", k, kshape, dt, device), _ld("v", v, kshape, dt, device),
+                 _ld("out", out, shape, dt, device), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                 _vector("q_off", q_off, i32, device, batch + 1), _vector("k_begin", k_begin, i32, device, batch),
+                 _vector("k_end", k_end, i32, device, batch))
     if workspace is None:
         need = ctypes.c_size_t()
-        _check(lib().dare_k_attention_packed_workspace(ref, ctypes.byref(need)))
+        st = lib().dare_k_attention_packed_workspace(call, need)
+        if st:
+            _check(st)
         if need.value:
             workspace = _scratch(need.value, q.device, stream)
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on cuda:%d" % device)
     pw, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _enqueue(device, stream, lib().dare_k_attention_packed, ref, pq, pk, pv, po, *offsets, pw, size)
+    _enqueue(device, stream, lib().dare_k_attention_packed, call, pw, size)
 
 
 def dare_k_attention_packed_workspace(dtype, batch, total_q, max_q, max_k, n_heads, n_kv_heads, head_dim):
     """Bytes of the workspace of a dare_k_attention_packed call of these sizes (0: none)."""
     wq, wk = n_heads * head_dim, n_kv_heads * head_dim
-    cfg = DarePackedConfig(ctypes.sizeof(DarePackedConfig), dtype, batch, total_q, 0, max_q, max_k, n_heads, n_kv_heads,
-                           head_dim, 0, 1.0, wq, wk, wk, wq)
+    call = _pack(_PACKED_CALL, dtype, batch, total_q, 0, max_q, max_k, n_heads, n_kv_heads, head_dim, 0, 1.0, wq, wk, wk, wq,
+                 *[0] * 7)
     need = ctypes.c_size_t()
-    _check(lib().dare_k_attention_packed_workspace(ctypes.byref(cfg), ctypes.byref(need)))
+    _check(lib().dare_k_attention_packed_workspace(call, ctypes.byref(need)))
     return need.value
 
 

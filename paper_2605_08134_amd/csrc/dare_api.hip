@@ -1116,49 +1116,49 @@ dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, in
   return launched(dtype == DARE_BF16 ? launch_gemm_bf16(g, s) : launch_gemm_f32(g, s), "dare_k_linear");
 }
 
-dare_status dare_k_rope(int dtype, int layout, int n_tokens, int head_dim, int rot_dim, const int32_t* pos, const double* freqs,
-                        float magnitude, const void* q, long ldq, void* q_out, long ldqo, int n_heads, const void* k, long ldk,
-                        void* k_out, long ldko, const void* v, long ldv, void* v_out, long ldvo, int n_kv_heads,
-                        const int32_t* rows, int out_rows, void* hip_stream) {
-  if (dtype != DARE_F32 && dtype != DARE_BF16) return refuse("unknown dtype");
-  if (layout != DARE_ROPE_HALF && layout != DARE_ROPE_PAIRS) return refuse("unknown layout");
-  if (n_tokens < 0 || !std::isfinite(magnitude)) return refuse("size or magnitude out of range");
-  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim) return refuse("rot_dim must be even, 2 .. head_dim");
-  if (head_dim < 8 || head_dim % 8 != 0 || head_dim > kRopeMaxDim) return unsupported("head_dim must be a multiple of 8 up to 256");
-  if (n_tokens == 0) return DARE_OK;
-  if (!pos || !freqs) return refuse("null pointer");
-  if ((uintptr_t)pos % 4 != 0 || (uintptr_t)freqs % 8 != 0) return refuse("pos or freqs not aligned");
+dare_status dare_k_rope(const dare_rope_call* call, void* hip_stream) {
+  if (!call || call->struct_size != sizeof(dare_rope_call)) return refuse("null call, or struct_size does not match this library");
+  const dare_rope_call& c = *call;
+  if (c.dtype != DARE_F32 && c.dtype != DARE_BF16) return refuse("unknown dtype");
+  if (c.layout != DARE_ROPE_HALF && c.layout != DARE_ROPE_PAIRS) return refuse("unknown layout");
+  if (c.n_tokens < 0 || !std::isfinite(c.magnitude)) return refuse("size or magnitude out of range");
+  if (c.rot_dim < 2 || c.rot_dim % 2 != 0 || c.rot_dim > c.head_dim) return refuse("rot_dim must be even, 2 .. head_dim");
+  if (c.head_dim < 8 || c.head_dim % 8 != 0 || c.head_dim > kRopeMaxDim)
+    return unsupported("head_dim must be a multiple of 8 up to 256");
+  if (c.n_tokens == 0) return DARE_OK;
+  if (!c.pos || !c.freqs) return refuse("null pointer");
+  if (((uintptr_t)c.pos | (uintptr_t)c.rows) % 4 != 0 || (uintptr_t)c.freqs % 8 != 0) return refuse("pos, rows or freqs not aligned");
   RopeArgs r{};
-  const void* x[3] = {q, k, v};
-  void* out[3] = {q_out, k_out, v_out};
-  const long ldx[3] = {ldq, ldk, ldv}, ldo[3] = {ldqo, ldko, ldvo};
-  const size_t esize = dtype == DARE_BF16 ? 2 : 4;
+  const void* x[3] = {c.q, c.k, c.v};
+  void* out[3] = {c.q_out, c.k_out, c.v_out};
+  const long ldx[3] = {c.ldq, c.ldk, c.ldv}, ldo[3] = {c.ldqo, c.ldko, c.ldvo};
+  const size_t esize = c.dtype == DARE_BF16 ? 2 : 4;
   for (int i = 0; i < 3; ++i) {
     if ((x[i] == nullptr) != (out[i] == nullptr)) return refuse("an input without its output, or the other way round");
     if (!x[i]) continue;
-    const int heads = i == 0 ? n_heads : n_kv_heads;
+    const int heads = i == 0 ? c.n_heads : c.n_kv_heads;
     if (heads < 1 || heads > 65535) return refuse("number of heads out of range");
-    if (ldx[i] < (long)heads * head_dim || ldo[i] < (long)heads * head_dim) return refuse("ld below the width of a row");
+    if (ldx[i] < (long)heads * c.head_dim || ldo[i] < (long)heads * c.head_dim) return refuse("ld below the width of a row");
     if (ldx[i] > kMaxLd || ldo[i] > kMaxLd) return unsupported("ld beyond 2^24");
     if (((uintptr_t)x[i] | (uintptr_t)out[i]) % esize != 0) return refuse("tensors not aligned to their elements");
-    if (x[i] == out[i] && (ldx[i] != ldo[i] || (i > 0 && rows))) return refuse("in place: the same ld, and no rows");
+    if (x[i] == out[i] && (ldx[i] != ldo[i] || (i > 0 && c.rows))) return refuse("in place: the same ld, and no rows");
     r.x[i] = x[i];
     r.out[i] = out[i];
     r.ldx[i] = ldx[i];
     r.ldo[i] = ldo[i];
     r.heads[i] = heads;
   }
-  if (rows && out_rows < 1) return refuse("rows without rows to write");
-  r.n = n_tokens;
-  r.dim = head_dim;
-  r.rot = rot_dim;
-  r.pairs = layout == DARE_ROPE_PAIRS;
-  r.pos = pos;
-  r.freqs = freqs;
-  r.rows = rows;
-  r.out_rows = out_rows;
-  r.magnitude = magnitude;
-  return launched(launch_rope(dtype, r, static_cast<hipStream_t>(hip_stream)), "dare_k_rope");
+  if (c.rows && c.out_rows < 1) return refuse("rows without rows to write");
+  r.n = c.n_tokens;
+  r.dim = c.head_dim;
+  r.rot = c.rot_dim;
+  r.pairs = c.layout == DARE_ROPE_PAIRS;
+  r.pos = c.pos;
+  r.freqs = c.freqs;
+  r.rows = c.rows;
+  r.out_rows = c.out_rows;
+  r.magnitude = c.magnitude;
+  return launched(launch_rope(c.dtype, r, static_cast<hipStream_t>(hip_stream)), "dare_k_rope");
 }
 
 dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scaling, double factor, double context, double low,
@@ -1187,8 +1187,8 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
 }
 
 namespace {
-dare_status check_packed(const dare_packed_config* c, PackedArgs* a) {
-  if (!c || c->struct_size != sizeof(dare_packed_config)) return refuse("null config, or struct_size does not match this library");
+dare_status check_packed(const dare_packed_call* c, PackedArgs* a) {
+  if (!c || c->struct_size != sizeof(dare_packed_call)) return refuse("null call, or struct_size does not match this library");
   if (c->dtype != DARE_F32 && c->dtype != DARE_BF16) return refuse("unknown dtype");
   if (c->batch < 0 || c->total_q < 0 || c->k_rows < 0 || c->max_q < 0 || c->max_k < 0 || c->causal_block < 0)
     return refuse("negative size");
@@ -1220,39 +1220,38 @@ dare_status check_packed(const dare_packed_config* c, PackedArgs* a) {
 }
 }  // namespace
 
-dare_status dare_k_attention_packed_workspace(const dare_packed_config* cfg, size_t* bytes) {
+dare_status dare_k_attention_packed_workspace(const dare_packed_call* call, size_t* bytes) {
   if (!bytes) return refuse("null pointer");
   PackedArgs a{};
-  const dare_status st = check_packed(cfg, &a);
-  *bytes = st == DARE_OK && a.batch > 0 && a.total_q > 0 ? packed_workspace_floats(cfg->dtype, a) * sizeof(float) : 0;
+  const dare_status st = check_packed(call, &a);
+  *bytes = st == DARE_OK && a.batch > 0 && a.total_q > 0 ? packed_workspace_floats(call->dtype, a) * sizeof(float) : 0;
   return st;
 }
 
-dare_status dare_k_attention_packed(const dare_packed_config* cfg, const void* q, const void* k, const void* v, void* out,
-                                    const int32_t* q_off, const int32_t* k_begin, const int32_t* k_end, void* workspace,
-                                    size_t workspace_bytes, void* hip_stream) {
+dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspace, size_t workspace_bytes, void* hip_stream) {
   PackedArgs a{};
-  const dare_status st = check_packed(cfg, &a);
+  const dare_status st = check_packed(call, &a);
   if (st != DARE_OK) return st;
+  const dare_packed_call& c = *call;
   if (a.batch == 0 || a.total_q == 0) return DARE_OK;
-  if (!q || !out || !q_off || !k_begin || !k_end || (a.k_rows > 0 && (!k || !v))) return refuse("null pointer");
-  if (!aligned(cfg->dtype, q, a.ldq) || !aligned(cfg->dtype, out, a.ldo) || !aligned(cfg->dtype, k, a.ldk) ||
-      !aligned(cfg->dtype, v, a.ldv))
+  if (!c.q || !c.out || !c.q_off || !c.k_begin || !c.k_end || (a.k_rows > 0 && (!c.k || !c.v))) return refuse("null pointer");
+  if (!aligned(c.dtype, c.q, a.ldq) || !aligned(c.dtype, c.out, a.ldo) || !aligned(c.dtype, c.k, a.ldk) ||
+      !aligned(c.dtype, c.v, a.ldv))
     return refuse("rows must lie on 16-byte boundaries");
-  if (((uintptr_t)q_off | (uintptr_t)k_begin | (uintptr_t)k_end) % 4 != 0) return refuse("offsets not aligned");
-  const size_t need = packed_workspace_floats(cfg->dtype, a) * sizeof(float);
+  if (((uintptr_t)c.q_off | (uintptr_t)c.k_begin | (uintptr_t)c.k_end) % 4 != 0) return refuse("offsets not aligned");
+  const size_t need = packed_workspace_floats(c.dtype, a) * sizeof(float);
   if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
     return refuse("workspace missing, too small or not on a 16-byte boundary");
-  a.q = q;
-  a.k = k;
-  a.v = v;
-  a.out = out;
-  a.q_off = q_off;
-  a.k_begin = k_begin;
-  a.k_end = k_end;
+  a.q = c.q;
+  a.k = c.k;
+  a.v = c.v;
+  a.out = c.out;
+  a.q_off = c.q_off;
+  a.k_begin = c.k_begin;
+  a.k_end = c.k_end;
   a.workspace = static_cast<float*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  return launched(cfg->dtype == DARE_BF16 ? launch_attn_packed_bf16(a, s) : launch_attn_packed_f32(a, s), "dare_k_attention_packed");
+  return launched(c.dtype == DARE_BF16 ? launch_attn_packed_bf16(a, s) : launch_attn_packed_f32(a, s), "dare_k_attention_packed");
 }
 
 }  // extern "C"

@@ -2,6 +2,7 @@
 attn_packed.h: the keys that a token sees, and how the work is cut."""
 import ctypes
 import os
+import struct
 import subprocess
 
 import pytest
@@ -45,25 +46,50 @@ def test_linear_of_no_rows_is_fine_without_tensors(L):
     assert L.dare_k_linear(*dict(LINEAR, m=0, a=None, out=None, wt=None).values(), None) == B.DARE_OK
 
 
-ROPE = dict(dtype=B.DARE_BF16, layout=0, n=3, d=64, rot=64, pos=P, freqs=P, mag=1.0, q=P, ldq=256, qo=2 * P, ldqo=256, h=4,
-            k=P, ldk=128, ko=2 * P, ldko=128, v=P, ldv=128, vo=2 * P, ldvo=128, kv=2, rows=P, out_rows=9)
+ROPE = dict(size=B._ROPE_CALL.size, dtype=B.DARE_BF16, layout=0, n=3, d=64, rot=64, h=4, kv=2, out_rows=9, mag=1.0, pos=P, freqs=P, rows=P,
+            q=P, k=P, v=P, qo=2 * P, ko=2 * P, vo=2 * P, ldq=256, ldk=128, ldv=128, ldqo=256, ldko=128, ldvo=128)
 
 
 @pytest.mark.parametrize("change,want", [
+    (dict(size=8), B.DARE_ERR_INVALID_ARG), (dict(rows=P + 2), B.DARE_ERR_INVALID_ARG),
     (dict(dtype=2), B.DARE_ERR_INVALID_ARG), (dict(layout=2), B.DARE_ERR_INVALID_ARG), (dict(n=-1), B.DARE_ERR_INVALID_ARG),
     (dict(rot=0), B.DARE_ERR_INVALID_ARG), (dict(rot=7), B.DARE_ERR_INVALID_ARG), (dict(rot=66), B.DARE_ERR_INVALID_ARG),
     (dict(d=260, rot=8), B.DARE_ERR_UNSUPPORTED), (dict(d=264, rot=8), B.DARE_ERR_UNSUPPORTED), (dict(d=4, rot=2), B.DARE_ERR_UNSUPPORTED),
-    (dict(pos=None), B.DARE_ERR_INVALID_ARG), (dict(freqs=None), B.DARE_ERR_INVALID_ARG), (dict(freqs=P + 4), B.DARE_ERR_INVALID_ARG),
+    (dict(pos=0), B.DARE_ERR_INVALID_ARG), (dict(freqs=0), B.DARE_ERR_INVALID_ARG), (dict(freqs=P + 4), B.DARE_ERR_INVALID_ARG),
     (dict(pos=P + 2), B.DARE_ERR_INVALID_ARG), (dict(mag=float("nan")), B.DARE_ERR_INVALID_ARG),
-    (dict(mag=float("inf")), B.DARE_ERR_INVALID_ARG), (dict(qo=None), B.DARE_ERR_INVALID_ARG), (dict(k=None), B.DARE_ERR_INVALID_ARG),
+    (dict(mag=float("inf")), B.DARE_ERR_INVALID_ARG), (dict(qo=0), B.DARE_ERR_INVALID_ARG), (dict(k=0), B.DARE_ERR_INVALID_ARG),
     (dict(ldq=255), B.DARE_ERR_INVALID_ARG), (dict(ldvo=127), B.DARE_ERR_INVALID_ARG), (dict(h=0), B.DARE_ERR_INVALID_ARG),
     (dict(kv=0), B.DARE_ERR_INVALID_ARG), (dict(q=P + 1), B.DARE_ERR_INVALID_ARG), (dict(k=2 * P), B.DARE_ERR_INVALID_ARG),
     (dict(q=2 * P, ldq=260), B.DARE_ERR_INVALID_ARG), (dict(out_rows=0), B.DARE_ERR_INVALID_ARG),
     (dict(ldq=(1 << 24) + 1), B.DARE_ERR_UNSUPPORTED),
 ])
 def test_rope_refuses(L, change, want):
-    assert L.dare_k_rope(*dict(ROPE, **change).values(), None) == want
+    assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, **change).values()), None) == want
     assert L.dare_last_error(None)
+
+
+def test_rope_of_no_call_and_of_no_tokens(L):
+    assert L.dare_k_rope(None, None) == B.DARE_ERR_INVALID_ARG
+    assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, n=0, q=0, pos=0, freqs=0).values()), None) == B.DARE_OK
+
+
+def test_structs_of_the_binding_are_those_of_the_header(tmp_path):
+    """Size and the place of the last field of every group."""
+    (tmp_path / "sizes.cpp").write_text(r"""
+#include <cstdio>
+#include <cstddef>
+#include "dare_kernels.h"
+#define P(t, f) std::printf("%zu ", offsetof(t, f))
+int main() {
+  std::printf("%zu %zu ", sizeof(dare_rope_call), sizeof(dare_packed_call));
+  P(dare_rope_call, magnitude); P(dare_rope_call, pos); P(dare_rope_call, rows); P(dare_rope_call, v); P(dare_rope_call, v_out); P(dare_rope_call, ldvo);
+  P(dare_packed_call, scale); P(dare_packed_call, ldo); P(dare_packed_call, out); P(dare_packed_call, k_end);
+}""")
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "include"), str(tmp_path / "sizes.cpp"), "-o", str(tmp_path / "sizes")], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()]
+    at = lambda fmt: struct.calcsize("@" + fmt)
+    assert got == [B._ROPE_CALL.size, B._PACKED_CALL.size, at("I8i"), at("I8ifP") - 8, at("I8if3P") - 8, at("I8if6P") - 8, at("I8if9P") - 8,
+                   B._ROPE_CALL.size - 8, at("I10i"), at("I10if4q") - 8, at("I10if4q4P") - 8, B._PACKED_CALL.size - 8]
 
 
 @pytest.mark.parametrize("args,want", [
@@ -78,10 +104,11 @@ def test_rope_freqs_refuses(L, args, want):
 
 
 def _packed(**kw):
-    base = dict(struct_size=ctypes.sizeof(B.DarePackedConfig), dtype=B.DARE_BF16, batch=2, total_q=5, k_rows=50, max_q=4, max_k=30,
-                n_heads=4, n_kv_heads=2, head_dim=64, causal_block=1, scale=0.125, ldq=256, ldk=128, ldv=128, ldo=256)
+    base = dict(struct_size=B._PACKED_CALL.size, dtype=B.DARE_BF16, batch=2, total_q=5, k_rows=50, max_q=4, max_k=30,
+                n_heads=4, n_kv_heads=2, head_dim=64, causal_block=1, scale=0.125, ldq=256, ldk=128, ldv=128, ldo=256,
+                q=P, k=P, v=P, out=P, q_off=P, k_begin=P, k_end=P)
     base.update(kw)
-    return B.DarePackedConfig(**base)
+    return B._PACKED_CALL.pack(*base.values())
 
 
 @pytest.mark.parametrize("kw,want", [
@@ -94,33 +121,30 @@ def _packed(**kw):
     (dict(batch=2 ** 24), B.DARE_ERR_UNSUPPORTED),
     (dict(batch=2 ** 23, n_heads=256, n_kv_heads=256, ldq=2 ** 14, ldk=2 ** 14, ldv=2 ** 14, ldo=2 ** 14), B.DARE_ERR_UNSUPPORTED),
 ])
-def test_attention_refuses_a_config(L, kw, want):
-    cfg, need = _packed(**kw), ctypes.c_size_t(7)
-    assert L.dare_k_attention_packed(ctypes.byref(cfg), P, P, P, P, P, P, P, P, 1 << 30, None) == want
+def test_attention_refuses_a_call(L, kw, want):
+    call, need = _packed(**kw), ctypes.c_size_t(7)
+    assert L.dare_k_attention_packed(call, P, 1 << 30, None) == want
     assert L.dare_last_error(None)
-    assert L.dare_k_attention_packed_workspace(ctypes.byref(cfg), ctypes.byref(need)) == want and need.value == 0
+    assert L.dare_k_attention_packed_workspace(call, ctypes.byref(need)) == want and need.value == 0
 
 
 def test_attention_refuses_pointers_and_workspaces(L):
-    ok = [P] * 7 + [P, 1 << 30]
-    call = lambda cfg, args: L.dare_k_attention_packed(ctypes.byref(cfg), *args, None)
-    for i in range(7):
-        assert call(_packed(), ok[:i] + [None] + ok[i + 1:]) == B.DARE_ERR_INVALID_ARG, i
-    for i in range(4):
-        assert call(_packed(), ok[:i] + [P + 8] + ok[i + 1:]) == B.DARE_ERR_INVALID_ARG, i
-    for i in range(4, 7):
-        assert call(_packed(), ok[:i] + [P + 2] + ok[i + 1:]) == B.DARE_ERR_INVALID_ARG, i
-    assert call(_packed(ldk=132), ok) == B.DARE_ERR_INVALID_ARG
+    run = lambda ws=P, size=1 << 30, **kw: L.dare_k_attention_packed(_packed(**kw), ws, size, None)
+    for name in ("q", "k", "v", "out", "q_off", "k_begin", "k_end"):
+        assert run(**{name: 0}) == B.DARE_ERR_INVALID_ARG, name
+        assert run(**{name: P + (8 if name in ("q", "k", "v", "out") else 2)}) == B.DARE_ERR_INVALID_ARG, name
+    assert run(ldk=132) == B.DARE_ERR_INVALID_ARG
     long = dict(batch=1, total_q=1, max_q=1, max_k=100000, k_rows=100000)
     need = ctypes.c_size_t()
-    assert L.dare_k_attention_packed_workspace(ctypes.byref(_packed(**long)), ctypes.byref(need)) == B.DARE_OK
+    assert L.dare_k_attention_packed_workspace(_packed(**long), ctypes.byref(need)) == B.DARE_OK
     assert need.value > 0
-    for ws in ([None, need.value], [P, need.value - 1], [P + 4, need.value]):
-        assert call(_packed(**long), [P] * 7 + ws) == B.DARE_ERR_INVALID_ARG
-    assert L.dare_k_attention_packed(None, *ok, None) == B.DARE_ERR_INVALID_ARG
-    assert L.dare_k_attention_packed_workspace(ctypes.byref(_packed()), None) == B.DARE_ERR_INVALID_ARG
+    for ws in ((None, need.value), (P, need.value - 1), (P + 4, need.value)):
+        assert run(*ws, **long) == B.DARE_ERR_INVALID_ARG
+    assert L.dare_k_attention_packed(None, P, 1 << 30, None) == B.DARE_ERR_INVALID_ARG
+    assert L.dare_k_attention_packed_workspace(_packed(), None) == B.DARE_ERR_INVALID_ARG
     # nothing to do: no pointers needed
-    assert call(_packed(total_q=0), [None] * 8 + [0]) == B.DARE_OK and call(_packed(batch=0), [None] * 8 + [0]) == B.DARE_OK
+    nothing = dict(q=0, k=0, v=0, out=0, q_off=0, k_begin=0, k_end=0)
+    assert run(None, 0, total_q=0, **nothing) == B.DARE_OK and run(None, 0, batch=0, **nothing) == B.DARE_OK
 
 
 def test_binding_refuses_what_is_not_on_the_gpu():
