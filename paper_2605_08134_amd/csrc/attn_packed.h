@@ -53,9 +53,10 @@ constexpr PackedPlan packed_plan(int batch, int total_q, int max_q, int max_k, i
   // (8 sequences of 300 keys uncut 10.6 us, in two parts 12.0), and fewer where 16 rounds of workgroups even out by themselves.  For
   // more than 256 sequences, whose lengths a workgroup does not look through, parts of 512.
   // Many rows, whose partial results are bytes that count: as many parts as give every CU two workgroups, or, up to four, four, because
-  // sequences differ and masked rows see less (32 tokens each over 32 caches of 100 to 4000 keys 98 us with two parts, 79 with
-  // four, 2000 causal ones 45 and 41, but 64 over 60000 keys 96 with 32 parts and 120 with 64); of 512 keys, or 256 where
-  // there are CUs to spare (32 tokens over 4000 keys 20.5 and 17.3, over 16 caches of 256 to 2048 36 and 43).
+  // sequences differ and masked rows see less (with equal parts: 32 tokens each over 32 caches of 100 to 4000 keys 98 us with two,
+  // 79 with four, 2000 causal ones 45 and 41, but 64 over 60000 keys 96 with 32 parts and 120 with 64; 62, 38 and 96 since the parts
+  // follow the lengths, Layout); of 512 keys, or 256 where there are CUs to spare (32 tokens over 4000 keys 20.5 and 17.3, over
+  // 16 caches of 256 to 2048 36 and 43).
   // (pairs: blocks that hold rows, about: at least what the rows fill, at least one of every sequence)
   const long filled = (long)total_q * group / plan.rows, some = batch < total_q ? batch : total_q;
   const long pairs = (filled > some ? filled : some > 0 ? some : 1) * n_kv;
