@@ -212,7 +212,7 @@ dare_status dare_k_rope(const dare_rope_call* call, void* hip_stream);
  *   DARE_ROPE_SCALE_TURNS   f_i (g + (1 - g) / factor), g = clamp((turns_i - low) / (high - low), 0, 1), turns_i = context f_i /
  *                           (2 pi): pairs that turn `high` times in the trained context stay, those that turn `low` times are interpolated
  * Computed on the HOST in double precision and copied to the device pointer `freqs` (fp64 [rot_dim / 2]) with a
- * synchronous copy.
+ * synchronous copy, which does not wait for other streams: nothing enqueued may still use the memory.
  */
 enum { DARE_ROPE_SCALE_NONE = 0, DARE_ROPE_SCALE_LINEAR = 1, DARE_ROPE_SCALE_BASE = 2, DARE_ROPE_SCALE_TURNS = 3 };
 dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scaling, double factor, double context,

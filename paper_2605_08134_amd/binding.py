@@ -631,6 +631,7 @@ def dare_k_rope_freqs(rot_dim, base=10000.0, scaling=None, factor=1.0, context=8
         raise ValueError("scaling must be one of %s" % list(ROPE_SCALINGS))
     freqs = torch.empty(max(rot_dim, 2) // 2, dtype=torch.float64, device=device)
     with torch.cuda.device(freqs.device):
+        torch.cuda.current_stream().synchronize()  # (the memory may have been that of a tensor still in use there)
         _check(lib().dare_k_rope_freqs(_ptr(freqs), rot_dim, float(base), ROPE_SCALINGS[scaling], float(factor),
                                        float(context), float(low), float(high)))
     return freqs

@@ -544,3 +544,23 @@ def test_layer_captured_and_replayed_with_other_lengths():
         assert torch.equal(y, want), rep
         assert torch.equal(cap.k, eager.k) and torch.equal(cap.v, eager.v)
         ctx = [c + 1 for c in ctx]
+
+
+def test_frequencies_in_memory_that_an_earlier_kernel_still_writes():
+    """Made while the stream still has work for a freed tensor whose memory they get: they come behind it."""
+    want = B.dare_k_rope_freqs(128).cpu()
+    busy = torch.empty(1 << 28, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            old = torch.empty(64, dtype=torch.float64, device="cuda")
+            for _ in range(20):
+                busy.fill_(1.0)
+            old.fill_(7.0)
+            del old
+            freqs = B.dare_k_rope_freqs(128)
+            side.synchronize()
+            assert torch.equal(freqs.cpu(), want)
+            del freqs
+    torch.cuda.synchronize()
