@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "attn_packed.h"
 #include "dare_common.h"
 
 using namespace dare;
@@ -1125,6 +1126,7 @@ dare_status dare_k_rope(const dare_rope_call* call, void* hip_stream) {
   if (c.rot_dim < 2 || c.rot_dim % 2 != 0 || c.rot_dim > c.head_dim) return refuse("rot_dim must be even, 2 .. head_dim");
   if (c.head_dim < 8 || c.head_dim % 8 != 0 || c.head_dim > kRopeMaxDim)
     return unsupported("head_dim must be a multiple of 8 up to 256");
+  if (c.n_tokens > 1 << 25) return unsupported("more than 2^25 tokens");
   if (c.n_tokens == 0) return DARE_OK;
   if (!c.pos || !c.freqs) return refuse("null pointer");
   if (((uintptr_t)c.pos | (uintptr_t)c.rows) % 4 != 0 || (uintptr_t)c.freqs % 8 != 0) return refuse("pos, rows or freqs not aligned");
@@ -1234,6 +1236,10 @@ dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspac
   if (st != DARE_OK) return st;
   const dare_packed_call& c = *call;
   if (a.batch == 0 || a.total_q == 0) return DARE_OK;
+  // (a workgroup of up to 256 lanes for a block of rows: a launch has fewer than 2^32 lanes)
+  const int group = a.n_heads / a.n_kv_heads;
+  const int rows = c.dtype == DARE_BF16 ? packed_plan(a.batch, a.total_q, a.max_q, a.max_k, group, a.n_kv_heads).rows : 16;
+  if (((long)a.total_q * group / rows + a.batch) * a.n_kv_heads >= 1l << 24) return unsupported("more than 2^24 blocks of rows");
   if (!c.q || !c.out || !c.q_off || !c.k_begin || !c.k_end || (a.k_rows > 0 && (!c.k || !c.v))) return refuse("null pointer");
   if (!aligned(c.dtype, c.q, a.ldq) || !aligned(c.dtype, c.out, a.ldo) || !aligned(c.dtype, c.k, a.ldk) ||
       !aligned(c.dtype, c.v, a.ldv))

@@ -250,3 +250,15 @@ def test_the_plan_covers_every_row_and_key(probe, batch, max_q, max_k, group, kv
     assert 1 <= parts <= 64 and keys * parts >= max_k
     if parts > 1:
         assert keys % 64 == 0 and keys >= 128 and -(-max_k // keys) <= parts
+
+
+def test_launches_of_more_lanes_than_there_can_be_are_refused(L):
+    """2^32 lanes in a launch: a workgroup of 256 per four tokens, per block of rows and key head."""
+    assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, n=(1 << 25) + 1).values()), None) == B.DARE_ERR_UNSUPPORTED
+    wide = dict(n_heads=8, n_kv_heads=8, ldq=512, ldk=512, ldv=512, ldo=512, batch=1, q=0)   # q=0: nothing is launched
+    for dtype, max_q, rows in ((B.DARE_BF16, 1, 16), (B.DARE_BF16, 32, 32), (B.DARE_BF16, 33, 128), (B.DARE_F32, 33, 16)):
+        for blocks, want in (((1 << 21) - 2, B.DARE_ERR_INVALID_ARG), (1 << 21, B.DARE_ERR_UNSUPPORTED)):
+            call = _packed(**dict(wide, dtype=dtype, max_q=max_q, total_q=min(blocks * rows, (1 << 28) - 17)))
+            if rows == 128:   # (the limit of 2^31 rows comes first)
+                want = B.DARE_ERR_INVALID_ARG
+            assert L.dare_k_attention_packed(call, P, 1 << 30, None) == want, (dtype, max_q, blocks)
