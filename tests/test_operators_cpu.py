@@ -258,7 +258,6 @@ def test_launches_of_more_lanes_than_there_can_be_are_refused(L):
     wide = dict(n_heads=8, n_kv_heads=8, ldq=512, ldk=512, ldv=512, ldo=512, batch=1, q=0)   # q=0: nothing is launched
     for dtype, max_q, rows in ((B.DARE_BF16, 1, 16), (B.DARE_BF16, 32, 32), (B.DARE_BF16, 33, 128), (B.DARE_F32, 33, 16)):
         for blocks, want in (((1 << 21) - 2, B.DARE_ERR_INVALID_ARG), (1 << 21, B.DARE_ERR_UNSUPPORTED)):
+            # (2^28 - 17 tokens of 8 heads stay below the limit on rows, and are (2^28 - 17) // 128 + 1 = 2^21 blocks of 128)
             call = _packed(**dict(wide, dtype=dtype, max_q=max_q, total_q=min(blocks * rows, (1 << 28) - 17)))
-            if rows == 128:   # (the limit of 2^31 rows comes first)
-                want = B.DARE_ERR_INVALID_ARG
             assert L.dare_k_attention_packed(call, P, 1 << 30, None) == want, (dtype, max_q, blocks)
