@@ -37,14 +37,20 @@ struct GemmF32Dev {
   int rope_cols, rope_dh, rope_seq;
   const uint8_t* sel_mask;  // row list made in the kernel, as in the bf16 path
   int sel_batch, sel_seq;
-  int32_t* sel_idx_out;
-  int32_t* sel_idx_out2;
-  int32_t* sel_off_out;
-  int32_t* sel_count_out;
-  const float* bias;        // act(product + bias) + residual (the LINEAR form)
-  const float* residual;
-  long ldr;
-  int act;
+  union {
+    struct {
+      int32_t* sel_idx_out;
+      int32_t* sel_idx_out2;
+      int32_t* sel_off_out;
+      int32_t* sel_count_out;
+    };
+    struct {  // act(product + bias) + residual (the LINEAR form, which makes no list)
+      const float* bias;
+      const float* residual;
+      long ldr;
+      int act;
+    };
+  };
 };
 
 // silu(z) = z / (1 + e^-z); gelu(z) = z Phi(z) = z erfc(-z / sqrt(2)) / 2; its tanh form z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3)
@@ -294,14 +300,17 @@ hipError_t launch_gemm_f32(const GemmArgs& g, hipStream_t s) {
   p.sel_mask = g.sel_mask;
   p.sel_batch = g.sel_batch;
   p.sel_seq = g.sel_seq;
-  p.sel_idx_out = g.sel_idx_out;
-  p.sel_idx_out2 = g.sel_idx_out2;
-  p.sel_off_out = g.sel_off_out;
-  p.sel_count_out = g.sel_count_out;
-  p.bias = static_cast<const float*>(g.bias);
-  p.residual = static_cast<const float*>(g.residual);
-  p.ldr = g.ldr;
-  p.act = g.act;
+  if (g.linear) {
+    p.bias = static_cast<const float*>(g.bias);
+    p.residual = static_cast<const float*>(g.residual);
+    p.ldr = g.ldr;
+    p.act = g.act;
+  } else {
+    p.sel_idx_out = g.sel_idx_out;
+    p.sel_idx_out2 = g.sel_idx_out2;
+    p.sel_off_out = g.sel_off_out;
+    p.sel_count_out = g.sel_count_out;
+  }
   if (p.sel_mask && (long)g.sel_batch * g.sel_seq > kSelMaxTokensF32) return hipErrorInvalidValue;
   if (g.linear) return launch_linear(p, s);
   // The largest tile that gives most of the chip's 256 CUs a workgroup.  Measured (us; before: 64 x 64
