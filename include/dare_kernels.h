@@ -232,6 +232,8 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
  *                outside of q, k and v is read, and nothing outside of out written.)
  * max_q and max_k, the largest numbers of query tokens and keys of a sequence, choose how the work is cut: a
  * captured call may be replayed with other lengths.  Longer sequences than they say are right as well, only slower.
+ * Logits, maxima and sums are held in fp32.  Probabilities go into the product with the values as fp32 in fp32; in bf16 to 2^-15 of each where
+ * max_q G is 32 or less (single tokens), and rounded to bf16 (2^-8 of each, the sum being taken over them as rounded) where it is more.
  * workspace: dare_k_attention_packed_workspace() bytes (for the same call; it does not look at the pointers), 16-byte aligned, needed while the call runs, not
  * initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, n_heads not a multiple of n_kv_heads, scale not above 0 or not

@@ -21,8 +21,10 @@
 //
 // Logits are formed transposed, S^T = K Q^T, with v_mfma_f32_16x16x32_bf16: a lane holds logits of one row, and the
 // probabilities are in the layout of the second operand of O^T = V^T P^T, whose first operand is read from the row-major
-// V tile by the LDS transpose read.  Running maximum (its reference, in base 2) and sum per row in fp32; probabilities are
-// rounded to bf16 for the value product, as the matrix cores take them, and the sum is taken over them as rounded.
+// V tile by the LDS transpose read.  Running maximum (its reference, in base 2) and sum per row in fp32.  The matrix cores take
+// probabilities in bf16.  With few rows, where they have little to do, a probability goes in as two of them, 2^-15 of it off at most
+// (Rows::softmax).  With many rows, where a second product would be half of the first two again, it is rounded to bf16 (2^-8 of it at
+// most), and the sum is taken over what is multiplied.
 //
 // Values in masked places do not count, whatever they are: a tile in which some row does not see some key multiplies with
 // those elements of V that are not finite replaced by 0, and adds what is not finite to the rows that see it.
@@ -97,10 +99,12 @@ __device__ __forceinline__ void load_rows(const bf16_t* base, long ld, int first
 }
 
 // 32 keys against R blocks of 16 rows.  kt, vt: LDS addresses of the keys' rows; key0: number of the first one.
-// MASKED: row r of a lane sees keys below lim[r] only.
-template <int DH, int R>
+// MASKED: row r of a lane sees keys below lim[r] only.  REST: probabilities in two parts.
+template <int DH, int R, bool REST>
 struct Rows {
   static constexpr int CB = DH / 16;  // 16-channel blocks
+  static constexpr int PARTS = REST ? 2 : 1;
+  static constexpr float kLift = 1.f / 65536;
   bf16x8 qf[R][DH / 32];
   f32x4 acc[CB][R];                   // channels 16 c + 4 kq .. + 3 of row l16
   float m[R], l[R];                   // reference in base 2, this lane's part of the sum
@@ -144,7 +148,10 @@ struct Rows {
 
   // The reference moves only when a maximum is 2^8 above it (any reference gives the same result up to rounding);
   // it stays finite, so a row that sees nothing has probabilities 0.
-  __device__ __forceinline__ void softmax(const f32x4 (&x)[R][2], bf16x8 (&pf)[R], float scale_log2) {
+  // REST: the first part of p is p cut to 8 bits, c; the second one is p - c + c / 2^16, rounded to 8 bits (it is 2^-7 p at most, its rounding
+  // 2^-15 p).  The lift is there because neither part may be 0 next to an infinite value (0 times infinity); what
+  // it adds is 2^-16 of every p to 2^-24, so the sum gets it too and the quotient none.
+  __device__ __forceinline__ void softmax(const f32x4 (&x)[R][2], bf16x8 (&pf)[PARTS][R], float scale_log2) {
     const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -166,18 +173,31 @@ struct Rows {
         f32x2 v;
         v[0] = __builtin_amdgcn_exp2f(fmaf(x[r][n >> 2][n & 3], scale_log2, -m[r]));
         v[1] = __builtin_amdgcn_exp2f(fmaf(x[r][n >> 2][(n & 3) + 1], scale_log2, -m[r]));
-        const bf16x2 pb = __builtin_convertvector(v, bf16x2);
-        sum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum, false);
-        pf[r][n] = pb[0];
-        pf[r][n + 1] = pb[1];
+        bf16x2 pb;
+        if constexpr (REST) {
+          const float p0 = v[0], p1 = v[1];  // (copied before their bits are taken, as in row_join)
+          sum += p0 + p1;
+          const unsigned bits[2] = {__builtin_bit_cast(unsigned, p0), __builtin_bit_cast(unsigned, p1)};
+          pb = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(bits[1], bits[0], 0x07060302u));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) v[i] = fmaf(__builtin_bit_cast(float, bits[i] & 0xffff0000u), kLift - 1.f, v[i]);
+          const bf16x2 rest = __builtin_convertvector(v, bf16x2);
+          pf[PARTS - 1][r][n] = rest[0];
+          pf[PARTS - 1][r][n + 1] = rest[1];
+        } else {
+          pb = __builtin_convertvector(v, bf16x2);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum, false);
+        }
+        pf[0][r][n] = pb[0];
+        pf[0][r][n + 1] = pb[1];
       }
-      l[r] += sum;
+      l[r] += REST ? sum * (1.f + kLift) : sum;
     }
   }
 
   // O^T += V^T P^T: slot s of a fragment is key 16 (s / 4) + 4 kq + s % 4
   template <bool MASKED>
-  __device__ __forceinline__ void values(unsigned vt, const bf16x8 (&pf)[R], int key0, int len_k) {
+  __device__ __forceinline__ void values(unsigned vt, const bf16x8 (&pf)[PARTS][R], int key0, int len_k) {
     constexpr int ROWB = DH * 2;
     const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
     const int key = kq * 4 + (l16 >> 2);
@@ -211,7 +231,14 @@ struct Rows {
     for (int c = 0; c < CB; ++c)
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]), pf[r], acc[c][r], 0, 0, 0);
+        acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]), pf[0][r], acc[c][r], 0, 0, 0);
+    if constexpr (REST) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]), pf[PARTS - 1][r], acc[c][r], 0, 0, 0);
+    }
   }
 
   // What is not finite among the values, to the rows that see it (their probability is above 0)
@@ -236,8 +263,8 @@ struct Rows {
 };
 
 // This lane's rows: row j of the sequence is token j / G, head j % G of the group; those past the last one repeat it.
-template <int DH, int R>
-__device__ __forceinline__ void take_rows(const PackedDev& p, const Place& at, int kvh, int row0, Rows<DH, R>& w, long (&out_at)[R]) {
+template <int DH, int R, bool REST>
+__device__ __forceinline__ void take_rows(const PackedDev& p, const Place& at, int kvh, int row0, Rows<DH, R, REST>& w, long (&out_at)[R]) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, kq = lane >> 4;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -297,7 +324,7 @@ __device__ __forceinline__ void few_rows(const PackedDev& p, const Place& at, in
     load_k(t + NW, 1);
     load_v(t + NW, 1);
   }
-  Rows<DH, R> w;
+  Rows<DH, R, true> w;
   long out_at[R];
   take_rows(p, at, kvh, 0, w, out_at);
   w.clear();
@@ -311,7 +338,7 @@ __device__ __forceinline__ void few_rows(const PackedDev& p, const Place& at, in
     const int key0 = t * kFewKeys;
     const bool masked = key0 + kFewKeys > least;
     f32x4 x[R][2];
-    bf16x8 pf[R];
+    bf16x8 pf[2][R];
     if (one) wait_vmcnt<3 * L>(); else wait_vmcnt<L>();
     w.logits(kt, x);
     wait_lds();
@@ -510,7 +537,7 @@ __device__ __forceinline__ void many_rows(const PackedDev& p, const Place& at, i
     load_tiles(Yes{}, 0);
   }
   if (n_steps > 1) load_tiles(No{}, 1);
-  Rows<DH, 2> w;
+  Rows<DH, 2, false> w;
   long out_at[2];
   take_rows(p, at, kvh, wave * 32, w, out_at);
   w.clear();
@@ -689,7 +716,7 @@ __device__ __forceinline__ void many_rows(const PackedDev& p, const Place& at, i
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         if (key + u * 32 >= ends) break;
-        bf16x8 pr[2];
+        bf16x8 pr[1][2];
         w.mask(x[u], key + u * 32);
         w.softmax(x[u], pr, p.scale_log2);
         w.template values<true>(vt + u * 32 * ROWB, pr, key + u * 32, at.len_k);

@@ -1,0 +1,64 @@
+"""Results of dare_k_linear and dare_k_attention_packed against bounds that leave no room for a rounding that their kernels do not make, and
+every tile shape of the projection."""
+import pytest
+import torch
+
+from paper_2605_08134_amd import binding as B
+import operator_util as ou
+
+pytestmark = pytest.mark.gpu
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ---- attention of few rows ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("h,kv,d,lq,lens", [
+    (1, 1, 128, 1, [64]), (8, 1, 128, 1, [300, 33, 129]), (4, 2, 64, 3, [150, 31, 257]), (16, 4, 128, 7, [260, 90]),    # 16 and 32 rows
+    (8, 2, 128, 1, [1400, 700]), (8, 2, 64, 4, [2000]),                                                               # keys cut
+    (4, 2, 128, 1, [200] * 70 + [1300] * 3), (2, 2, 64, 1, [90] * 300),                            # more than 64 and than 256 sequences
+])
+@pytest.mark.parametrize("block", [0, 1])
+def test_attention_of_few_rows_keeps_its_probabilities(h, kv, d, lq, lens, block):
+    """A probability is taken in two parts of 8 bits, so that its product with a value is off by 2^-15 of it (what the second part, at most
+    2^-7 of the whole where the first one is cut off, loses by its own rounding, 2^-8 of that); the rest of the bound is that of the fp32 path."""
+    g = _gen(h * 1000 + d + len(lens))
+    off, kb = [i * lq for i in range(len(lens) + 1)], [0]
+    for n in lens:
+        kb.append(kb[-1] + n)
+    q = ou.rand(g, off[-1], h, d, dtype="bf16", std=0.25)
+    k, v = ou.rand(g, kb[-1], kv, d, dtype="bf16"), ou.rand(g, kb[-1], kv, d, dtype="bf16")
+    scale = d ** -0.5
+    want, bound, _ = ou.attention64(q.float(), k.float(), v.float(), off, kb[:-1], kb[1:], block, scale)
+    mean, _, _ = ou.attention64(q.float(), k.float(), v.float().abs(), off, kb[:-1], kb[1:], block, scale)
+    bound = bound + 2.0 ** -15 * mean
+    bound = bound + 2.0 ** -8 * (want.abs() + bound)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    B.dare_k_attention_packed(q.cuda(), k.cuda(), v.cuda(), out, ints(off), ints(kb[:-1]), ints(kb[1:]), lq, max(lens), causal_block=block)
+    assert ou.worst(out, want, bound) <= 1.0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_few_rows_over_values_that_are_not_finite(d):
+    """An infinity or a NaN among the values that a token sees is in its own channel of the result, and there only."""
+    g = _gen(d)
+    q, k, v = (ou.rand(g, n, x, d, dtype="bf16").cuda() for n, x in ((2, 4), (500, 2), (500, 2)))
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+
+    def run(v):
+        out = torch.empty_like(q)
+        B.dare_k_attention_packed(q, k, v, out, ints([0, 2]), ints([0]), ints([500]), 2, 500)
+        return out
+
+    clean = run(v)
+    v2 = v.clone()
+    v2[7, 0, 3], v2[300, 0, 5], v2[499, 0, 9] = float("inf"), float("-inf"), float("nan")
+    v2[20, 1, 30], v2[21, 1, 30] = float("inf"), float("-inf")
+    got = run(v2)
+    assert (got[:, :2, 3] == float("inf")).all() and (got[:, :2, 5] == float("-inf")).all() and torch.isnan(got[:, :2, 9]).all()
+    assert torch.isnan(got[:, 2:, 30]).all()
+    rest = torch.isfinite(got)
+    assert torch.equal(got[rest], clean[rest]) and int((~rest).sum()) == 2 * (2 * 3 + 2)
