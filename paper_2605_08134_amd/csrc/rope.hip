@@ -188,7 +188,7 @@ hipError_t launch_layout(RopeDev p, const int (&heads)[3], bool pairs, bool alig
 }  // namespace
 
 hipError_t launch_rope(int dtype, const RopeArgs& a, hipStream_t s) {
-  if (a.n == 0) return hipSuccess;
+  if (a.n == 0 || (!a.x[0] && !a.x[1] && !a.x[2])) return hipSuccess;
   RopeDev p{};
   const size_t esize = dtype == DARE_BF16 ? 2 : 4;
   uintptr_t bits = 0;  // of all that lies on 16 bytes or does not

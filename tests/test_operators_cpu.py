@@ -73,6 +73,13 @@ def test_rope_of_no_call_and_of_no_tokens(L):
     assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, n=0, q=0, pos=0, freqs=0).values()), None) == B.DARE_OK
 
 
+@pytest.mark.parametrize("rows", [0, P])
+def test_rope_without_tensors_has_nothing_to_do(L, rows):
+    """q, k and v may each be left out, and so may all of them: nothing is launched."""
+    none = dict(q=0, k=0, v=0, qo=0, ko=0, vo=0)
+    assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, rows=rows, **none).values()), None) == B.DARE_OK
+
+
 def test_structs_of_the_binding_are_those_of_the_header(tmp_path):
     """Size and the place of the last field of every group."""
     (tmp_path / "sizes.cpp").write_text(r"""
