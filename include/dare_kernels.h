@@ -167,7 +167,7 @@ enum { DARE_ACT_NONE = 0, DARE_ACT_SILU = 1, DARE_ACT_GELU = 2, DARE_ACT_GELU_TA
  *   a [m, lda], residual [m, ldr] (or NULL), out [m, ldo] dtype; wt [n, k] (packed weight), bias [n] (or NULL) dtype
  * out may be residual (with the same ld); it must not overlap a.  k and n are multiples of 64.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, unknown act), UNSUPPORTED (k or n not a
- * multiple of 64).
+ * multiple of 64, m beyond 2^24, n beyond 2^20, an ld beyond 2^24).
  */
 dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, int n, int k, int m, const void* bias,
                           int act, const void* residual, long ldr, void* out, long ldo, void* hip_stream);
@@ -184,8 +184,11 @@ dare_status dare_k_linear(int dtype, const void* a, long lda, const void* wt, in
  *   rows   NULL: k_out and v_out have a row per token.  Else [n_tokens] int32: token t goes to row rows[t] of them, nowhere if that is
  *          outside [0, out_rows); no two tokens to the same row
  * Each of q, k and v may be NULL (with its output).  q_out may be q, and without rows k_out k and v_out v (with the same
- * ld); there is no other overlap.  head_dim is a multiple of 8 up to 256, rot_dim even, 2 .. head_dim, n_tokens up to
- * 2^25.  Rows need no alignment but that of their elements.
+ * ld); there is no other overlap.  head_dim is a multiple of 8 up to 256, rot_dim even, 2 .. head_dim, heads 1 .. 65535, n_tokens up to
+ * 2^25, an ld up to 2^24.  Rows need no alignment but that of their elements.
+ * Errors: INVALID_ARG (struct_size, null pointer, an input without its output, ld below the row's width, alignment, in place with rows or another ld,
+ * rows without out_rows, unknown dtype or layout, magnitude not finite, rot_dim, heads out of range), UNSUPPORTED (head_dim, n_tokens or an ld
+ * beyond what is said here).
  */
 enum { DARE_ROPE_HALF = 0, DARE_ROPE_PAIRS = 1 };
 typedef struct {
@@ -237,9 +240,10 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
  * workspace: dare_k_attention_packed_workspace() bytes (for the same call; it does not look at the pointers), 16-byte aligned, needed while the call runs, not
  * initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, n_heads not a multiple of n_kv_heads, scale not above 0 or not
- * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; total_q * n_heads + 128 batch beyond
+ * finite, workspace too small), UNSUPPORTED (head_dim not 64 or 128; an ld beyond 2^24; total_q * n_heads + 128 batch beyond
  * 2^31; 2^24 blocks and more, of n_kv_heads (total_q G / R + batch), R = 16 in fp32, else 16, 32 or 128: the smallest that max_q G rows fit,
- * or 128).
+ * or 128).  The query of the workspace looks neither at pointers nor at the number of blocks, and refuses what else the call
+ * refuses.
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_packed_call) */

@@ -268,3 +268,22 @@ def test_launches_of_more_lanes_than_there_can_be_are_refused(L):
             # (2^28 - 17 tokens of 8 heads stay below the limit on rows, and are (2^28 - 17) // 128 + 1 = 2^21 blocks of 128)
             call = _packed(**dict(wide, dtype=dtype, max_q=max_q, total_q=min(blocks * rows, (1 << 28) - 17)))
             assert L.dare_k_attention_packed(call, P, 1 << 30, None) == want, (dtype, max_q, blocks)
+
+
+def test_limits_that_the_header_names(L):
+    """Every ld up to 2^24, heads of a rotation up to 65535; the query of the workspace does not count blocks."""
+    beyond = (1 << 24) + 64
+    for change in (dict(lda=beyond), dict(ldo=beyond), dict(residual=3 * P, ldr=beyond)):
+        assert L.dare_k_linear(*dict(LINEAR, **change).values(), None) == B.DARE_ERR_UNSUPPORTED, change
+    for name in ("ldq", "ldk", "ldv", "ldqo", "ldko", "ldvo"):
+        assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, **{name: beyond}).values()), None) == B.DARE_ERR_UNSUPPORTED, name
+    for change in (dict(h=65536, ldq=1 << 23, ldqo=1 << 23), dict(kv=65536, ldk=1 << 23, ldko=1 << 23)):
+        assert L.dare_k_rope(B._ROPE_CALL.pack(*dict(ROPE, **change).values()), None) == B.DARE_ERR_INVALID_ARG
+    need = ctypes.c_size_t(7)
+    for name in ("ldq", "ldk", "ldv", "ldo"):
+        call = _packed(**{name: beyond})
+        assert L.dare_k_attention_packed(call, P, 1 << 30, None) == B.DARE_ERR_UNSUPPORTED, name
+        assert L.dare_k_attention_packed_workspace(call, ctypes.byref(need)) == B.DARE_ERR_UNSUPPORTED and need.value == 0
+    many = _packed(n_heads=8, n_kv_heads=8, ldq=512, ldk=512, ldv=512, ldo=512, batch=1 << 21, max_q=1, total_q=5)
+    assert L.dare_k_attention_packed(many, P, 1 << 30, None) == B.DARE_ERR_UNSUPPORTED
+    assert L.dare_k_attention_packed_workspace(many, ctypes.byref(need)) == B.DARE_OK
