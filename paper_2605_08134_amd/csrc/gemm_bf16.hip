@@ -158,8 +158,10 @@ __device__ __forceinline__ float silu(float g) {
 
 // Activation of N values at once: what it is is settled outside the loop.  Reciprocals and exponentials by the hardware's
 // instructions, 1 ulp of fp32 each, behind them a rounding to bf16.
-// GELU: z Phi(z) = max(z, 0) - |z| erfc(|z| / sqrt(2)) / 2 with erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2), t = 1 / (1 + p x)
-// (Abramowitz and Stegun, 7.1.26), 1.5e-7 off at most, in 14 instructions.
+// GELU: z Phi(z) = max(z, 0) - |z| h(|z|) e^(-z^2 / 2), h(x) = e^(x^2 / 2) erfc(x / sqrt(2)) / 2 = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))), t = 1 / (1 +
+// p x), in 14 instructions.  p and the a_i are a fit of our own (least largest error of h relative to min(e^(1.2 x), 400), by linear
+// programming): evaluated in fp32 the result is off by 7e-7 at most and, where it falls to 0, by 4.7e-4 of itself, an eighth of the rounding to
+// bf16, down to z = -13, where it ends.  (One term more: 1e-7 and 1.3e-4, but 16384 x 12288 x 4096 1225 us for 1212, x 4096 x 512 136 for 130.)
 // Tanh form: z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
 template <int N>
 __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
@@ -170,11 +172,11 @@ __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float z = v[i], x = fabsf(z);
-      const float t = __builtin_amdgcn_rcpf(fmaf(x, 0.231641888f, 1.f));
-      float e = fmaf(t, 0.5307027145f, -0.7265760135f);
-      e = fmaf(t, e, 0.7107068705f);
-      e = fmaf(t, e, -0.142248368f);
-      e = fmaf(t, e, 0.127414796f) * t * __builtin_amdgcn_exp2f(-0.72134752f * x * x);
+      const float t = __builtin_amdgcn_rcpf(fmaf(x, 0.35056123f, 1.f));
+      float e = fmaf(t, -0.096569724f, 0.27045822f);
+      e = fmaf(t, e, 0.024472961f);
+      e = fmaf(t, e, 0.16388455f);
+      e = fmaf(t, e, 0.13775338f) * t * __builtin_amdgcn_exp2f(-0.72134752f * x * x);
       v[i] = fmaf(-fminf(x, 1e18f), e, fmaxf(z, 0.f));  // (infinity times 0 is none)
     }
   } else if (act == DARE_ACT_GELU_TANH) {

@@ -62,3 +62,27 @@ def test_attention_of_few_rows_over_values_that_are_not_finite(d):
     assert torch.isnan(got[:, 2:, 30]).all()
     rest = torch.isfinite(got)
     assert torch.equal(got[rest], clean[rest]) and int((~rest).sum()) == 2 * (2 * 3 + 2)
+
+
+# ---- activations of the projection ----------------------------------------------------------------
+
+def _act64(act, z):
+    """ou.act64 with nothing cancelled where the result is small."""
+    if act == "gelu":
+        return z * torch.special.erfc(-z / 2 ** 0.5) / 2
+    if act == "gelu_tanh":
+        return z * torch.special.expit(2 * (2 / torch.pi) ** 0.5 * (z + 0.044715 * z ** 3))
+    return ou.act64(act, z)
+
+
+@pytest.mark.parametrize("act,least", [("silu", -80.0), ("gelu", -12.5), ("gelu_tanh", -8.0)])
+@pytest.mark.parametrize("m", [5, 20, 40])
+def test_linear_activations_far_below_zero(act, least, m):
+    """An activation that falls towards 0 is right relative to itself: the rounding to bf16, 2^-8 at most, and what the fp32 form is off by,
+    2^-11 (an exponential whose argument of up to 80 is rounded three times, 80 x 3 x 2^-24; the fit of the erf form 4.7e-4)."""
+    z = -torch.logspace(-3, 0, m * 64, dtype=torch.float64).mul(-least).view(m, 64).bfloat16()
+    z[m // 2] = -z[m // 2]
+    out = torch.empty(m, 64, dtype=torch.bfloat16, device="cuda")
+    B.dare_k_linear(z.cuda(), torch.eye(64, dtype=torch.bfloat16, device="cuda"), out, act=act)
+    want = _act64(act, z.double())
+    assert ou.worst(out, want, (2.0 ** -8 + 2.0 ** -11) * want.abs()) <= 1.0
