@@ -164,6 +164,7 @@ enum { DARE_ACT_NONE = 0, DARE_ACT_SILU = 1, DARE_ACT_GELU = 2, DARE_ACT_GELU_TA
  * Projection with its epilogue, one rounding at the end:
  *     out[t, 0:n] = act(a[t, 0:k] . W + bias) + residual[t, 0:n]        for t in [0, m)
  * act: none; silu z / (1 + e^-z); gelu z Phi(z); its tanh form z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.
+ * Of -infinity gelu is 0, the others are NaN, in both types.
  *   a [m, lda], residual [m, ldr] (or NULL), out [m, ldo] dtype; wt [n, k] (packed weight), bias [n] (or NULL) dtype
  * out may be residual (with the same ld); it must not overlap a.  k and n are multiples of 64.
  * Errors: INVALID_ARG (null pointer, ld below the row's width, alignment, unknown act), UNSUPPORTED (k or n not a

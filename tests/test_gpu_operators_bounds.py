@@ -86,3 +86,18 @@ def test_linear_activations_far_below_zero(act, least, m):
     B.dare_k_linear(z.cuda(), torch.eye(64, dtype=torch.bfloat16, device="cuda"), out, act=act)
     want = _act64(act, z.double())
     assert ou.worst(out, want, (2.0 ** -8 + 2.0 ** -11) * want.abs()) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [3, 30, 300])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_linear_activations_of_infinities(dtype, m, act):
+    """The same in both types and every kernel: infinity of infinity; of -infinity 0 (gelu) or NaN, infinity over infinity; no other row changes."""
+    x = ou.rand(_gen(m), m, 64, dtype=dtype)
+    x[:, 0], x[m // 2, 0], x[m - 1, 0], x[0, 0] = 0.0, float("inf"), float("-inf"), float("nan")
+    w = torch.ones(64, 64, dtype=x.dtype)
+    out, bias, res = torch.empty(m, 64, dtype=x.dtype, device="cuda"), torch.ones(64, dtype=x.dtype), torch.full((m, 64), 3.0, dtype=x.dtype)
+    B.dare_k_linear(x.cuda(), w.cuda(), out, bias.cuda(), act, res.cuda())
+    assert ((out[m - 1] == 3) if act == "gelu" else torch.isnan(out[m - 1])).all() and (out[m // 2] == float("inf")).all() and torch.isnan(out[0]).all()
+    rest = [i for i in range(m) if i not in (0, m // 2, m - 1)]
+    assert torch.isfinite(out[rest]).all()
