@@ -1576,7 +1576,7 @@ __device__ __forceinline__ void skinny_tile(const GemmDev& p, const int m, unsig
     __syncthreads();
   }
 }
-constexpr int kSkinnyRows = 32, kSkinnyMaxN = 8192;
+constexpr int kSkinnyRows = 32;
 
 // ---- one tile shape, chosen on the host (row count known): k in ranges, then whole k --------------
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
@@ -2170,13 +2170,7 @@ hipError_t launch_rows_wide(const GemmArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The shapes of the plain projection by its rule, but for few rows, where the CUs that have a tile pull the operands:
-//   * up to 8 rows of narrow outputs: the stream over the weights, one workgroup per 16 columns.  It pulls every row once per 16
-//     columns and in pieces of 64 bytes, so with more rows tiles are faster: n x k = 4096 x 4096, 4096 x 12288, 2176 x 9408, 448 x 4352, 8 rows 9.3
-//     28.9 16.8 8.1 us, 16 rows 10.6 34.1 19.7 10.0, 32 rows 14.4 45.0 29.7 18.4;
-//   * up to 32 rows of narrow outputs: 32 x 32 in eight stages (16 rows 9.6 32.7 17.0 9.0, 32 rows 9.7 36.1 17.2 9.1, with sixteen
-//     stages 10.4 36.8 17.8 9.5; 32 x 64 13.2 52.1 23.9 12.4);
-//   * as long as 64 x 64 leave half of the CUs without a tile: 64 x 32 (64 rows, 64 x 64 and this, 14.9 13.4, 63.3 49.0, 28.3 24.1).
+// act(A W + bias) + residual (linear_route)
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 hipError_t launch_linear_tile16(const GemmArgs& g, hipStream_t s) {
   hipLaunchKernelGGL((linear_bf16_tile16_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>),
@@ -2200,13 +2194,12 @@ hipError_t launch_linear_quad(const GemmArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_linear(const GemmArgs& g, hipStream_t s) {
-  if (g.m_max <= 8 && g.n < kSkinnyMaxN) {
-    hipLaunchKernelGGL(linear_bf16_skinny_kernel, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
-    return hipGetLastError();
-  }
-  if (g.m_max <= 32 && g.n < kSkinnyMaxN) return launch_linear_tile16<32, 32, 2, 2, 8>(g, s);
-  if (tiles_of(g.m_max, g.n, 64, 64) <= 128) return launch_linear_tile16<64, 32, 4, 2, 6>(g, s);
-  switch (gemm_route(g.m_max, g.n, g.k, 1, false)) {
+  switch (linear_route(g.m_max, g.n, g.k)) {
+    case GemmRoute::kSkinny:
+      hipLaunchKernelGGL(linear_bf16_skinny_kernel, dim3(g.n / 16), dim3(512), 0, s, to_dev(g));
+      return hipGetLastError();
+    case GemmRoute::k32x32: return launch_linear_tile16<32, 32, 2, 2, 8>(g, s);
+    case GemmRoute::k64x32: return launch_linear_tile16<64, 32, 4, 2, 6>(g, s);
     case GemmRoute::kQuad256: return launch_linear_quad<4>(g, s);
     case GemmRoute::kQuad192: return launch_linear_quad<3>(g, s);
     case GemmRoute::kPp256: return launch_linear_pp<4>(g, s);

@@ -23,6 +23,9 @@ enum class GemmRoute {
   kPp128Split,  // 256 x 128, two workgroups on the halves of a tile's k; needs the workspace
   kQuad192,     // 256 rows x 192, 256 columns: four waves, one pipeline over a workgroup's tiles (all rows)
   kQuad256,
+  kSkinny,      // no tiles: a stream over the weights, one workgroup per 16 columns (few rows)
+  k32x32,       // with an epilogue, few rows
+  k64x32,
 };
 
 constexpr int kRouteBK = 64;        // k per k-step
@@ -153,6 +156,22 @@ constexpr long part_tiles(int m, int n, int part_m, int part_n, int tn) {
 }
 __attribute__((always_inline)) constexpr int part_columns(int m, int n, int part_m, int part_n) {
   return quad_cost(part_tiles(m, n, part_m, part_n, 3), 3) < quad_cost(part_tiles(m, n, part_m, part_n, 4), 4) ? 3 : 4;
+}
+
+// All rows with act(product + bias) + residual as the epilogue: the shapes of the plain projection by its rule, but for few rows, where the
+// CUs that have a tile pull the operands:
+//   * up to 8 rows of narrow outputs: the stream over the weights, one workgroup per 16 columns.  It pulls every row once per 16
+//     columns and in pieces of 64 bytes, so with more rows tiles are faster: n x k = 4096 x 4096, 4096 x 12288, 2176 x 9408, 448 x 4352, 8 rows 9.3
+//     28.9 16.8 8.1 us, 16 rows 10.6 34.1 19.7 10.0, 32 rows 14.4 45.0 29.7 18.4;
+//   * up to 32 rows of narrow outputs: 32 x 32 in eight stages (16 rows 9.6 32.7 17.0 9.0, 32 rows 9.7 36.1 17.2 9.1, with sixteen
+//     stages 10.4 36.8 17.8 9.5; 32 x 64 13.2 52.1 23.9 12.4);
+//   * as long as 64 x 64 leave half of the CUs without a tile: 64 x 32 (64 rows, 64 x 64 and this, 14.9 13.4, 63.3 49.0, 28.3 24.1).
+constexpr int kSkinnyMaxN = 8192;
+constexpr GemmRoute linear_route(int m, int n, int k) {
+  if (n < kSkinnyMaxN && m <= 8) return GemmRoute::kSkinny;
+  if (n < kSkinnyMaxN && m <= 32) return GemmRoute::k32x32;
+  if (tiles_of(m, n, 64, 64) <= 128) return GemmRoute::k64x32;
+  return gemm_route(m, n, k, 1, false);
 }
 
 // What a launch of `tiles` tiles takes where it is compared with one of another number of tiles: rounds of the CUs above all, idle CUs

@@ -104,3 +104,14 @@ def worst(got, want, bound):
     share = ((got - want).abs() / (bound + 1e-30)).nan_to_num(0.0)
     share[bad] = math.inf
     return float(share.max()) if share.numel() else 0.0
+
+
+# dare_k_linear in bf16: (route, rows, columns, k), every route of its launch, ragged in rows and, but for the first three, in the columns of the tile
+LINEAR_SHAPES = [
+    ("kSkinny", 5, 448, 4352), ("k32x32", 19, 320, 4160), ("k64x32", 65, 1088, 1024), ("k64x64", 65, 4160, 2112), ("k64x96", 65, 8320, 1088),
+    ("k64x128", 65, 12352, 576), ("k64x128", 1, 126464, 192), ("k128x96", 130, 11008, 960), ("k128x128", 130, 12352, 704),
+    ("k128x192", 258, 11008, 1024), ("kPp128", 386, 8256, 2048), ("kPp192", 514, 11008, 1024), ("kPp256", 770, 12352, 1024),
+    ("kQuad192", 1026, 13120, 192), ("kQuad256", 1538, 14144, 192),
+    ("kQuad256", 770, 12352, 4160),      # one round of tiles, a long k
+    ("kQuad256", 4617, 15424, 192),      # more than 128 MB of outputs, which are stored past the L2
+]

@@ -41,7 +41,7 @@ def test_linear(act, dtype, m, n, k, extras):
     assert ou.worst(out, want, bound) <= 1.0
 
 
-# one size per tile shape of many rows (256 CUs), ragged in rows and columns
+# many rows, ragged in rows and columns (every tile shape: test_gpu_operators_bounds.py)
 @pytest.mark.parametrize("m,n,k", [(515, 1600, 128), (777, 6144, 128), (1000, 2112, 192), (1100, 4096, 64), (1281, 8256, 256),
                                    (2047, 3136, 128), (2049, 4160, 448), (4100, 4416, 128), (9000, 1216, 64)])
 @pytest.mark.parametrize("act,extras", [(None, False), ("gelu", True)])

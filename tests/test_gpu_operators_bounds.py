@@ -101,3 +101,37 @@ def test_linear_activations_of_infinities(dtype, m, act):
     assert ((out[m - 1] == 3) if act == "gelu" else torch.isnan(out[m - 1])).all() and (out[m // 2] == float("inf")).all() and torch.isnan(out[0]).all()
     rest = [i for i in range(m) if i not in (0, m // 2, m - 1)]
     assert torch.isfinite(out[rest]).all()
+
+
+# ---- every tile shape of the projection -------------------------------------------------------------
+
+@pytest.mark.parametrize("route,m,n,k", ou.LINEAR_SHAPES)
+@pytest.mark.parametrize("act,extras", [(None, "none"), ("gelu", "both"), ("silu", "in place")])
+def test_linear_in_every_tile_shape(route, m, n, k, act, extras):
+    """Rows of a, residual and output that end in something else; the sampled rows against 64 bits, all of them against fp32, the ends of the
+    output's rows as they were."""
+    g = torch.Generator(device="cuda").manual_seed(m)
+    rn = lambda *s: torch.randn(s, device="cuda", generator=g).bfloat16()
+    a, wt, bias = rn(m, k + 64), rn(n, k).mul_(k ** -0.5), rn(n) if extras != "none" else None
+    a[:, k:] = float("nan")
+    a, buf, res = a[:, :k], torch.full((m, n + 8), 7.0, dtype=torch.bfloat16, device="cuda"), None
+    out = buf[:, :n]
+    if extras == "both":
+        res = rn(m, n + 16)[:, :n]
+        before = res
+    elif extras == "in place":
+        before = rn(m, n)
+        out.copy_(before)
+        res = out
+    B.dare_k_linear(a, wt, out, bias, act, res)
+    assert (buf[:, n:] == 7).all()
+    rows = torch.cat([torch.arange(0, m, 97), torch.tensor([m - 1])])
+    want, bound = ou.linear64(a[rows.cuda()].cpu(), wt.cpu(), None if bias is None else bias.cpu(), act,
+                              None if res is None else before[rows.cuda()].cpu())
+    assert ou.worst(out[rows.cuda()], want, bound) <= 1.0
+    full = a.float() @ wt.float().t() + (0.0 if bias is None else bias.float())
+    # (both sums in fp32: twice the bound that ou.linear64 has for one)
+    slack = 2.26 * (k + 2) * ou.U32 * (a.float().abs() @ wt.float().abs().t() + 4.0) + 2.0 ** -19 * (full.abs() + 1)
+    full = full if act is None else torch.nn.functional.gelu(full) if act == "gelu" else torch.nn.functional.silu(full)
+    full = full if res is None else full + before.float()
+    assert ((out.float() - full).abs() <= 2.0 ** -8 * (full.abs() + slack) + slack).all()

@@ -287,3 +287,39 @@ def test_limits_that_the_header_names(L):
     many = _packed(n_heads=8, n_kv_heads=8, ldq=512, ldk=512, ldv=512, ldo=512, batch=1 << 21, max_q=1, total_q=5)
     assert L.dare_k_attention_packed(many, P, 1 << 30, None) == B.DARE_ERR_UNSUPPORTED
     assert L.dare_k_attention_packed_workspace(many, ctypes.byref(need)) == B.DARE_OK
+
+
+ROUTES = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <initializer_list>
+#include "gemm_route.h"
+int main(int n, char** a) {
+  for (int i = 1; i + 2 < n; i += 3) std::printf("%d ", (int)dare::linear_route(atoi(a[i]), atoi(a[i + 1]), atoi(a[i + 2])));
+  if (n > 1) return 0;
+  bool seen[64] = {};  // what the rule ever takes
+  for (int m = 1; m <= 20000; m = m < 300 ? m + 1 : m + m / 37)
+    for (int c = 64; c <= 1 << 20; c = c < 16384 ? c + 64 : c + c / 640 * 64)
+      for (int k : {64, 128, 192, 2048, 4096}) seen[(int)dare::linear_route(m, c, k)] = true;
+  for (int r = 0; r < 64; ++r)
+    if (seen[r]) std::printf("%d ", r);
+}
+"""
+
+
+def test_every_tile_shape_of_the_projection_has_a_test(tmp_path):
+    """The sizes that the GPU test runs take the routes that they are there for, those are all that the launch can take, and the rule takes no
+    other."""
+    import re
+    csrc = os.path.join(ROOT, "paper_2605_08134_amd", "csrc")
+    header, source = (open(os.path.join(csrc, f)).read() for f in ("gemm_route.h", "gemm_bf16.hip"))
+    names = re.findall(r"^  (k\w+),", header[header.index("enum class GemmRoute"):header.index("};")], re.M)
+    body = source[source.index("hipError_t launch_linear(const GemmArgs& g"):]
+    launched = set(re.findall(r"case GemmRoute::(\w+)", body[:body.index("default:")]))
+    (tmp_path / "routes.cpp").write_text(ROUTES)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", csrc, str(tmp_path / "routes.cpp"), "-o", str(tmp_path / "routes")], check=True)
+    run = lambda *args: [names[int(v)] for v in subprocess.run([str(tmp_path / "routes"), *args], capture_output=True, text=True, check=True).stdout.split()]
+    assert run(*[str(v) for s in ou.LINEAR_SHAPES for v in s[1:]]) == [s[0] for s in ou.LINEAR_SHAPES]
+    assert {s[0] for s in ou.LINEAR_SHAPES} == launched
+    assert set(run()) == launched
+    assert any(s[0] == "kQuad256" and s[1] * s[2] * 2 > 128 << 20 for s in ou.LINEAR_SHAPES)
