@@ -135,3 +135,21 @@ def test_linear_in_every_tile_shape(route, m, n, k, act, extras):
     full = full if act is None else torch.nn.functional.gelu(full) if act == "gelu" else torch.nn.functional.silu(full)
     full = full if res is None else full + before.float()
     assert ((out.float() - full).abs() <= 2.0 ** -8 * (full.abs() + slack) + slack).all()
+
+
+@pytest.mark.parametrize("act,least", [("silu", -80.0), ("gelu", -12.0), ("gelu_tanh", -8.0)])
+@pytest.mark.parametrize("m", [3, 40, 700])
+def test_linear_activations_in_fp32(act, least, m):
+    """With an identity the product is exact, and the activation's own errors are left, counted in roundings (2^-24) of the result: those of
+    the last operations and of the library's exponential and erfc (16 units in the last place, 32 roundings, are what OpenCL allows for
+    the latter, 3 for the former), and the argument's, as far as the function passes them on: silu's is exact; erfc of x passes on a relative
+    error 2 x^2 + 1 times, x = z / sqrt(2) rounded twice; the tanh form's exponent w is made of six rounded steps."""
+    z = torch.logspace(-6, 0, m * 64, dtype=torch.float64).mul(least).view(m, 64).float()
+    z[1::2] = -z[1::2]
+    out = torch.empty(m, 64, device="cuda")
+    B.dare_k_linear(z.cuda(), torch.eye(64, device="cuda"), out, act=act)
+    x = z.double()
+    want = _act64(act, x)
+    steps = {"silu": torch.full_like(x, 8.0), "gelu": 36.0 + 2 * (x ** 2 + 1),
+             "gelu_tanh": 10.0 + 6 * (1.6 * (x + 0.044715 * x ** 3)).abs()}[act]
+    assert ou.worst(out, want, steps * ou.U32 * want.abs()) <= 1.0
