@@ -674,6 +674,8 @@ def dare_k_rope(pos, freqs, layout="half", q=None, q_out=None, k=None, k_out=Non
             pv, ldv = v.data_ptr(), _ld("v", v, shape, dt, device)
             pvo, ldvo = v_out.data_ptr(), _ld("v_out", v_out, out_shape, dt, device)
     pr = 0 if rows is None else _vector("rows", rows, torch.int32, device, n)
+    if freqs.dim() != 1:
+        raise ValueError("freqs must be a vector, not %s" % (tuple(freqs.shape),))
     half = freqs.shape[0]
     call = _pack(_ROPE_CALL, code, ROPE_LAYOUTS[layout], n, d, 2 * half, 0 if q is None else h, kv, out_rows, magnitude,
                  _vector("pos", pos, torch.int32, device, n), _vector("freqs", freqs, torch.float64, device, half), pr,
@@ -694,6 +696,8 @@ def dare_k_attention_packed(q, k, v, out, q_off, k_begin, k_end, max_q, max_k, c
     if len(shape) != 3 or len(kshape) != 3 or shape[2] != kshape[2]:
         raise ValueError("q and k must be [tokens, heads, head_dim], not %s and %s" % (tuple(shape), tuple(kshape)))
     total, h, d = shape
+    if k_begin.dim() != 1:
+        raise ValueError("k_begin must be a vector, not %s" % (tuple(k_begin.shape),))
     batch = k_begin.shape[0]
     call = _pack(_PACKED_CALL, code, batch, total, kshape[0], max_q, max_k, h, kshape[1], d, causal_block,
                  d ** -0.5 if scale is None else scale,

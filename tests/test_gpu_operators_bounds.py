@@ -153,3 +153,21 @@ def test_linear_activations_in_fp32(act, least, m):
     steps = {"silu": torch.full_like(x, 8.0), "gelu": 36.0 + 2 * (x ** 2 + 1),
              "gelu_tanh": 10.0 + 6 * (1.6 * (x + 0.044715 * x ** 3)).abs()}[act]
     assert ou.worst(out, want, steps * ou.U32 * want.abs()) <= 1.0
+
+
+# ---- what the binding refuses -----------------------------------------------------------------------
+
+def test_vectors_without_a_length_are_refused():
+    one = torch.zeros((), dtype=torch.int32, device="cuda")
+    x = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    i = torch.zeros(4, dtype=torch.int32, device="cuda")
+    freqs = B.dare_k_rope_freqs(64)
+    for p, f in ((i, freqs[0]), (one, freqs), (i, freqs[None])):
+        with pytest.raises(ValueError):
+            B.dare_k_rope(p, f, "half", x, x)
+    with pytest.raises(ValueError):
+        B.dare_k_attention_packed(x, x, x, x.clone(), i, one, one, 1, 1)
+    for call in (lambda: B.dare_k_attention_packed(x, x, x, x.clone(), i, i[:3], i[:3], 1, 1, scale=1e39),
+                 lambda: B.dare_k_rope(i, freqs, "half", x, x, magnitude=1e39)):
+        with pytest.raises(B.DareError):      # beyond fp32: infinite
+            call()
