@@ -12,7 +12,8 @@
 // wave reads all lengths and lays the blocks and their parts out (Layout).  Else sequence b gets the block numbers from
 // floor(rows in front of it / BM) + b on, which is never less than the blocks that it needs: a workgroup finds its sequence by a search over
 // q_off, no sum over the sequences in front of it, and the grid is at most a block per sequence larger than a perfect
-// one.  The last blocks start first: under a causal mask they are the longest.
+// one.  Of a sequence the last blocks start first, under a causal mask its longest ones; the sequences start by their number, the last one
+// first, whatever their lengths.
 //
 // What bounds it.  Few rows: the bytes of K and V (one token over 131072 keys of 8 heads 98 to 104 us, 5.2 to 5.5 TB/s, and 6 for joining),
 // with short caches the latencies of two launches (10 us).  Many rows: issue (matrix cores busy 47 % of the CU cycles of twelve prompts of 33 to
@@ -23,8 +24,10 @@
 // probabilities are in the layout of the second operand of O^T = V^T P^T, whose first operand is read from the row-major
 // V tile by the LDS transpose read.  Running maximum (its reference, in base 2) and sum per row in fp32.  The matrix cores take
 // probabilities in bf16.  With few rows, where they have little to do, a probability goes in as two of them, 2^-15 of it off at most
-// (Rows::softmax).  With many rows, where a second product would be half of the first two again, it is rounded to bf16 (2^-8 of it at
-// most), and the sum is taken over what is multiplied.
+// (Rows::softmax; us, rounded and in two parts: one token over 131072 keys 108.8 and 108.6, over each of 64 caches up to 8000 205.5 and 205.3, 8 over
+// each of 16 up to 2000 25.3 and 25.7).  With many rows, where a second product is half of the first two again, it is rounded to bf16 (2^-8 of it
+// at most), and the sum is taken over what is multiplied (4 x 4096 tokens 950 and 1252, 16384 causal 1868 and 2466, blocks of 32 over 16 caches up to
+// 2048 32.5 and 36.6).
 //
 // Values in masked places do not count, whatever they are: a tile in which some row does not see some key multiplies with
 // those elements of V that are not finite replaced by 0, and adds what is not finite to the rows that see it.
@@ -765,7 +768,7 @@ __device__ __forceinline__ void many_rows(const PackedDev& p, const Place& at, i
   }
 }
 
-// A workgroup per block (and part: more than 256 sequences), the longest first
+// A workgroup per block (and part: more than 256 sequences), the last one first
 template <int DH>
 __global__ void __launch_bounds__(kManyWaves * 64, 2) attn_packed_many_kernel(PackedDev p) {
   __shared__ __attribute__((aligned(1024))) ManyShared<DH> shared;

@@ -166,6 +166,10 @@ __attribute__((always_inline)) constexpr int part_columns(int m, int n, int part
 //   * up to 32 rows of narrow outputs: 32 x 32 in eight stages (16 rows 9.6 32.7 17.0 9.0, 32 rows 9.7 36.1 17.2 9.1, with sixteen
 //     stages 10.4 36.8 17.8 9.5; 32 x 64 13.2 52.1 23.9 12.4);
 //   * as long as 64 x 64 leave half of the CUs without a tile: 64 x 32 (64 rows, 64 x 64 and this, 14.9 13.4, 63.3 49.0, 28.3 24.1).
+// Narrow: below 8192 columns, as in the plain projection.  On the other side, with 1, 8, 16 and 32 rows, k = 4096, these shapes and (in brackets) the
+// two for few rows as if there were no limit: 8192 columns 18.8 17.7 17.8 18.0 (16.5 19.9 15.0 15.6), 12288 23.0 21.6 22.4 23.3 (23.2
+// 28.6 22.9 25.1), 32000 56.4 56.2 56.3 56.6 (54.9 67.8 53.2 57.9), 126464 182 185 188 190 (204 258 183 207).  On this side, 7936 columns, 8 rows
+// 19.8 in the stream and 12 rows 14.6 in 32 x 32: near the limit the stream ends too late.
 constexpr int kSkinnyMaxN = 8192;
 constexpr GemmRoute linear_route(int m, int n, int k) {
   if (n < kSkinnyMaxN && m <= 8) return GemmRoute::kSkinny;
