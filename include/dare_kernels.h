@@ -229,7 +229,7 @@ dare_status dare_k_rope_freqs(double* freqs, int rot_dim, double base, int scali
  * over the keys that the token sees: all of its sequence with causal_block = 0; else those whose position lies in its own
  * block of causal_block positions or in one before (1: causal).  A token that sees no key gets zeros.  What lies in
  * keys that a token does not see does not matter, infinities and NaN included.
- *   q, out       [total_q, ldq or ldo] dtype, n_heads heads of head_dim
+ *   q, out       [total_q, ldq or ldo] dtype, n_heads heads of head_dim; out overlaps none of the inputs
  *   k, v         [k_rows, ldk or ldv] dtype, n_kv_heads heads: packed like the queries, or a cache
  *   q_off        [batch + 1] int32, ascending from 0; rows of out from q_off[batch] on are left as they are
  *   k_begin/end  [batch] int32, 0 <= begin <= end <= k_rows.  (Values outside are taken as the nearest inside, so nothing
