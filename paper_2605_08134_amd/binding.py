@@ -31,6 +31,7 @@ EXPORTS = (
     "dare_model_set_prefix", "dare_model_step", "dare_model_logits", "dare_model_layer",
     "dare_model_destroy", "dare_model_last_error",
     "dare_k_linear", "dare_k_rope", "dare_k_rope_freqs", "dare_k_attention_packed", "dare_k_attention_packed_workspace",
+    "dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs",
 )
 RULE_SCORE, RULE_QUANTILE = 0, 1
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
@@ -176,6 +177,9 @@ def lib():
     L.dare_k_quantile_mask.argtypes = [vp, i32, i32, f32, i32, vp, vp, vp, vp, vp]
     L.dare_k_quantile_mask.restype = i32
     lng = ctypes.c_long
+    for name in ("dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs"):
+        getattr(L, name).argtypes = [vp, vp]
+        getattr(L, name).restype = i32
     L.dare_k_linear.argtypes = [i32, vp, lng, vp, i32, i32, i32, vp, i32, vp, lng, vp, lng, vp]
     L.dare_k_linear.restype = i32
     L.dare_k_rope.argtypes = [vp, vp]
@@ -726,6 +730,82 @@ def dare_k_attention_packed_workspace(dtype, batch, total_q, max_q, max_k, n_hea
     need = ctypes.c_size_t()
     _check(lib().dare_k_attention_packed_workspace(call, ctypes.byref(need)))
     return need.value
+
+
+# ---- 8-bit codes, and the output end of a step --------------------------------------------
+
+# dare_norm_q8_call: struct_size, dtype, kind, n_rows, d; eps; ldx, ldo, ldxo, ldc; x, o, gain, bias, x_out, codes, scales
+_NORM_Q8_CALL = struct.Struct("@I4id4q7P")
+# dare_linear_q8_call: struct_size, dtype, m, n, k, act; lda, ldr, ldo; a, row_scale, wt, col_scale, bias, residual, out
+_LINEAR_Q8_CALL = struct.Struct("@I5i3q7P")
+# dare_logprobs_call: struct_size, dtype, n_rows, vocab, top, scale; ld; logits, tokens, logprobs, entropy, top_ids, top_logprobs
+_LOGPROBS_CALL = struct.Struct("@I4ifq6P")
+
+
+def dare_k_norm_q8(kind, x, codes, scales, o=None, x_out=None, gain=None, bias=None, eps=1e-5, stream=None):
+    """Rows of s = x + o (stored in x_out) or of their norm as 8-bit codes with a scale each: codes[t] * scales[t] stands for the
+    row.  kind None, "layer" or "rms"; x, o, x_out [rows, d], codes int8 [rows, d] with contiguous rows, scales float32 [rows], gain and
+    bias [d].  x_out may be x or o.  Codes of a weight: kind None of the packed one (dare_k_pack_weight), a scale per column."""
+    import torch
+    if x.dim() != 2 or kind not in NORM_KINDS:
+        raise ValueError("x must be a matrix, kind one of %s" % list(NORM_KINDS))
+    device, dt, code = _gpu_of(x)
+    rows, d = x.shape
+    px, ldx = _matrix("x", x, dt, device, rows, d)
+    po, ldo = (0, 0) if o is None else _matrix("o", o, dt, device, rows, d)
+    ps, lds = (0, 0) if x_out is None else _matrix("x_out", x_out, dt, device, rows, d)
+    pc, ldc = _matrix("codes", codes, torch.int8, device, rows, d)
+    call = _pack(_NORM_Q8_CALL, code, NORM_KINDS[kind], rows, d, eps, ldx, ldo, lds, ldc, px, po,
+                 0 if gain is None else _vector("gain", gain, dt, device, d),
+                 0 if bias is None else _vector("bias", bias, dt, device, d), ps, pc,
+                 _vector("scales", scales, torch.float32, device, rows))
+    _enqueue(device, stream, lib().dare_k_norm_q8, call)
+
+
+def dare_k_linear_q8(a, a_scales, wt, wt_scales, out, bias=None, act=None, residual=None, stream=None):
+    """out = act(a_scales wt_scales (a W) + bias) + residual.  a int8 [m, k] with contiguous rows, wt int8 [n, k] (the codes of a packed
+    weight), a_scales float32 [m], wt_scales float32 [n]; bias [n], residual and out [m, n] bfloat16 or float32; act None, "silu", "gelu" or
+    "gelu_tanh"; out may be residual."""
+    import torch
+    device, dt, code = _gpu_of(out)
+    if wt.dim() != 2 or a.dim() != 2 or act not in ACTIVATIONS:
+        raise ValueError("a and wt must be matrices, act one of %s" % list(ACTIVATIONS))
+    n, k = wt.shape
+    m = a.shape[0]
+    i8, f32 = torch.int8, torch.float32
+    pa, lda = _matrix("a", a, i8, device, m, k)
+    pw, ldw = _matrix("wt", wt, i8, device, n, k)
+    if ldw != k:
+        raise ValueError("wt must be contiguous")
+    po, ldo = _matrix("out", out, dt, device, m, n)
+    pr, ldr = (0, 0) if residual is None else _matrix("residual", residual, dt, device, m, n)
+    call = _pack(_LINEAR_Q8_CALL, code, m, n, k, ACTIVATIONS[act], lda, ldr, ldo, pa, _vector("a_scales", a_scales, f32, device, m), pw,
+                 _vector("wt_scales", wt_scales, f32, device, n), 0 if bias is None else _vector("bias", bias, dt, device, n), pr, po)
+    _enqueue(device, stream, lib().dare_k_linear_q8, call)
+
+
+def dare_k_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, scale=1.0, stream=None):
+    """Of p = softmax(scale logits) per row of logits [rows, vocab]: logprobs = log p of tokens (int32 [rows]), the entropy, and ids and
+    log-probabilities of the largest (top_ids int32, top_logprobs [rows, top], top up to 32; equal logits by their ids).  What is not
+    wanted is None; outputs are float32 [rows]."""
+    import torch
+    if logits.dim() != 2 or (top_ids is None) != (top_logprobs is None) or (top_ids is not None and top_ids.dim() != 2):
+        raise ValueError("logits must be a matrix, top_ids and top_logprobs both matrices or None")
+    device, dt, code = _gpu_of(logits)
+    rows, vocab = logits.shape
+    px, ld = _matrix("logits", logits, dt, device, rows, vocab)
+    i32, f32 = torch.int32, torch.float32
+    top = 0 if top_ids is None else top_ids.shape[1]
+    pi = pt = 0
+    if top_ids is not None:
+        pi, ldi = _matrix("top_ids", top_ids, i32, device, rows, top)
+        pt, ldt = _matrix("top_logprobs", top_logprobs, f32, device, rows, top)
+        if ldi != top or ldt != top:
+            raise ValueError("top_ids and top_logprobs must be contiguous")
+    call = _pack(_LOGPROBS_CALL, code, rows, vocab, top, scale, ld, px, 0 if tokens is None else _vector("tokens", tokens, i32, device, rows),
+                 0 if logprobs is None else _vector("logprobs", logprobs, f32, device, rows),
+                 0 if entropy is None else _vector("entropy", entropy, f32, device, rows), pi, pt)
+    _enqueue(device, stream, lib().dare_k_logprobs, call)
 
 
 def _scratch(n_bytes, device, stream):

@@ -1260,4 +1260,115 @@ dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspac
   return launched(c.dtype == DARE_BF16 ? launch_attn_packed_bf16(a, s) : launch_attn_packed_f32(a, s), "dare_k_attention_packed");
 }
 
+// ---- 8-bit codes, and the output end of a step --------------------------------------------------
+
+dare_status dare_k_norm_q8(const dare_norm_q8_call* call, void* hip_stream) {
+  if (!call || call->struct_size != sizeof(dare_norm_q8_call)) return refuse("null call, or struct_size does not match this library");
+  const dare_norm_q8_call& c = *call;
+  if (c.dtype != DARE_F32 && c.dtype != DARE_BF16) return refuse("unknown dtype");
+  if (c.kind < DARE_NORM_NONE || c.kind > DARE_NORM_RMS) return refuse("unknown norm kind");
+  if (c.n_rows < 0 || c.d < 1) return refuse("size out of range");
+  if (c.kind != DARE_NORM_NONE && !(c.eps >= 0.0 && std::isfinite(c.eps))) return refuse("eps must be >= 0");
+  if (c.d % 8 != 0) return unsupported("d must be a multiple of 8");
+  if (c.n_rows > 1 << 23 || c.d > kMaxLd) return unsupported("more than 2^23 rows, or rows of more than 2^24 channels");
+  if (c.ldx < c.d || c.ldc < c.d || (c.o && c.ldo < c.d) || (c.x_out && c.ldxo < c.d)) return refuse("ld below the width of a row");
+  if (c.ldx > kMaxLd || c.ldc > kMaxLd || (c.o && c.ldo > kMaxLd) || (c.x_out && c.ldxo > kMaxLd)) return unsupported("ld beyond 2^24");
+  if (c.n_rows == 0) return DARE_OK;
+  if (!c.x || !c.codes || !c.scales || (c.kind != DARE_NORM_NONE && !c.gain)) return refuse("null pointer");
+  if (c.kind == DARE_NORM_NONE && c.gain) return refuse("a gain without a norm");
+  if (c.kind != DARE_NORM_LAYER && c.bias) return refuse("bias is for LayerNorm only");
+  if (!aligned(c.dtype, c.x, c.ldx) || (c.o && !aligned(c.dtype, c.o, c.ldo)) || (c.x_out && !aligned(c.dtype, c.x_out, c.ldxo)) ||
+      !aligned(c.dtype, c.gain, 0) || !aligned(c.dtype, c.bias, 0))
+    return refuse("rows must lie on 16-byte boundaries");
+  if (((uintptr_t)c.codes | (uintptr_t)c.ldc) % 8 != 0 || (uintptr_t)c.scales % 4 != 0)
+    return refuse("codes must lie on 8-byte boundaries, scales on those of a float");
+  if ((c.x_out == c.x && c.ldxo != c.ldx) || (c.x_out && c.x_out == c.o && c.ldxo != c.ldo)) return refuse("a sum in the place of an input has its ld");
+  NormQ8Args a{};
+  a.x = c.x;
+  a.o = c.o;
+  a.x_out = c.x_out;
+  a.gain = c.gain;
+  a.bias = c.bias;
+  a.codes = c.codes;
+  a.scales = c.scales;
+  a.ldx = c.ldx;
+  a.ldo = c.ldo;
+  a.ldxo = c.ldxo;
+  a.ldc = c.ldc;
+  a.eps = c.eps;
+  a.kind = c.kind;
+  a.rows = c.n_rows;
+  a.d = c.d;
+  return launched(launch_norm_q8(c.dtype, a, static_cast<hipStream_t>(hip_stream)), "dare_k_norm_q8");
+}
+
+dare_status dare_k_linear_q8(const dare_linear_q8_call* call, void* hip_stream) {
+  if (!call || call->struct_size != sizeof(dare_linear_q8_call)) return refuse("null call, or struct_size does not match this library");
+  const dare_linear_q8_call& c = *call;
+  if (c.dtype != DARE_F32 && c.dtype != DARE_BF16) return refuse("unknown dtype");
+  if (c.m < 0 || c.n < 1 || c.k < 1) return refuse("size out of range");
+  if (c.act < DARE_ACT_NONE || c.act > DARE_ACT_GELU_TANH) return refuse("unknown activation");
+  if (c.n % 64 != 0 || c.k % 128 != 0) return unsupported("n must be a multiple of 64, k of 128");
+  if (c.k >= 1 << 17) return unsupported("k of 2^17 and more: sums beyond 32 bits");
+  if (c.m > 1 << 24 || c.n > 1 << 20 || (long)c.m * c.n > 1l << 37) return unsupported("more than 2^24 rows, 2^20 columns or 2^37 outputs");
+  if (c.m == 0) return DARE_OK;
+  if (!c.a || !c.row_scale || !c.wt || !c.col_scale || !c.out) return refuse("null pointer");
+  if (c.lda < c.k || c.ldo < c.n || (c.residual && c.ldr < c.n)) return refuse("ld below the width of a row");
+  if (c.lda > kMaxLd || c.ldo > kMaxLd || (c.residual && c.ldr > kMaxLd)) return unsupported("ld beyond 2^24");
+  if (((uintptr_t)c.a | (uintptr_t)c.lda | (uintptr_t)c.wt) % 16 != 0 || !aligned(c.dtype, c.out, c.ldo) || !aligned(c.dtype, c.bias, 0) ||
+      (c.residual && !aligned(c.dtype, c.residual, c.ldr)) || (uintptr_t)c.col_scale % 16 != 0)
+    return refuse("rows, bias and the columns' scales must lie on 16-byte boundaries");
+  if ((uintptr_t)c.row_scale % 4 != 0) return refuse("scales not aligned");
+  if (c.residual && c.residual == c.out && c.ldr != c.ldo) return refuse("a residual in the place of the output has its ld");
+  LinearQ8Args a{};
+  a.a = c.a;
+  a.row_scale = c.row_scale;
+  a.wt = c.wt;
+  a.col_scale = c.col_scale;
+  a.bias = c.bias;
+  a.residual = c.residual;
+  a.out = c.out;
+  a.lda = c.lda;
+  a.ldr = c.ldr;
+  a.ldo = c.ldo;
+  a.m = c.m;
+  a.n = c.n;
+  a.k = c.k;
+  a.act = c.act;
+  return launched(launch_linear_q8(c.dtype, a, static_cast<hipStream_t>(hip_stream)), "dare_k_linear_q8");
+}
+
+dare_status dare_k_logprobs(const dare_logprobs_call* call, void* hip_stream) {
+  if (!call || call->struct_size != sizeof(dare_logprobs_call)) return refuse("null call, or struct_size does not match this library");
+  const dare_logprobs_call& c = *call;
+  if (c.dtype != DARE_F32 && c.dtype != DARE_BF16) return refuse("unknown dtype");
+  if (c.n_rows < 0 || c.vocab < 1) return refuse("size out of range");
+  if (c.top < 0 || c.top > c.vocab) return refuse("top must be 0 .. vocab");
+  if (!(c.scale > 0.f) || !(c.scale <= 1e30f)) return refuse("scale must be above 0 and at most 1e30");
+  if (c.top > kTopMost) return unsupported("more than 32 alternatives");
+  if (c.n_rows > 1 << 21 || c.vocab > 1 << 28) return unsupported("more than 2^21 rows or 2^28 logits in a row");
+  if (c.ld < c.vocab) return refuse("ld below the width of a row");
+  if (c.ld > 1l << 32) return unsupported("ld beyond 2^32");
+  if (c.n_rows == 0) return DARE_OK;
+  if (!c.logits || (c.top > 0 && (!c.top_ids || !c.top_logprobs))) return refuse("null pointer");
+  if ((c.tokens == nullptr) != (c.logprobs == nullptr)) return refuse("tokens and their log-probabilities go together");
+  if ((uintptr_t)c.logits % (c.dtype == DARE_BF16 ? 2 : 4) != 0 ||
+      ((uintptr_t)c.tokens | (uintptr_t)c.logprobs | (uintptr_t)c.entropy | (uintptr_t)c.top_ids | (uintptr_t)c.top_logprobs) % 4 != 0)
+    return refuse("tensors must lie on the boundaries of their elements");
+  LogprobsArgs a{};
+  a.logits = c.logits;
+  a.ld = c.ld;
+  a.rows = c.n_rows;
+  a.vocab = c.vocab;
+  a.top = c.top;
+  a.scale = c.scale;
+  a.tokens = c.tokens;
+  a.logprobs = c.logprobs;
+  a.entropy = c.entropy;
+  a.top_ids = c.top_ids;
+  a.top_logprobs = c.top_logprobs;
+  if (!a.logprobs && !a.entropy && a.top == 0) return DARE_OK;
+  return launched(launch_logprobs(c.dtype, a, static_cast<hipStream_t>(hip_stream)), "dare_k_logprobs");
+}
+
 }  // extern "C"

@@ -100,6 +100,15 @@ __device__ __forceinline__ void rope_rotate4(const f32x4 cs, float& v0, float& v
   v3 = a3;
 }
 
+// Activations of the fp32 outputs (DARE_ACT_*): silu(z) = z / (1 + e^-z); gelu(z) = z Phi(z) = z erfc(-z / sqrt(2)) / 2; its tanh form z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
+// Of -infinity gelu is 0, as in bf16; the others are the quotient of two infinities there.
+__device__ __forceinline__ float activate_f32(int act, float z) {
+  if (act == DARE_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == DARE_ACT_GELU) return 0.5f * (z == -INFINITY ? -__FLT_MAX__ : z) * erfcf(-0.70710678f * z);  // (next to a 0)
+  if (act == DARE_ACT_GELU_TANH) return z / (1.f + expf(-1.59576912f * fmaf(0.044715f * z * z, z, z)));
+  return z;
+}
+
 // Drift score of one token from the sums <q, p>, |q|^2, |p|^2 (Sec. 3.1 eq. 1)
 __device__ __forceinline__ float drift_score(float dot, float nq, float np) {
   return 1.0f - dot / fmaxf(sqrtf(nq * np), 1e-30f);
@@ -161,6 +170,50 @@ constexpr int kAttnParts = 256;  // parts of a launch, at most: one per CU
 constexpr size_t attn_parts_elems(int head_dim) { return (size_t)kAttnParts * 64 * 2 * (head_dim / 2 + 2); }
 hipError_t launch_attn_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t s);
+
+// Projection of 8-bit codes with scales per row and column (dare_k_linear_q8)
+struct LinearQ8Args {
+  const int8_t* a;           // [*, lda]
+  const float* row_scale;    // [m]
+  const int8_t* wt;          // [n, k]
+  const float* col_scale;    // [n]
+  const void* bias;          // [n] or nullptr
+  const void* residual;      // [*, ldr] or nullptr
+  void* out;                 // [*, ldo]
+  long lda, ldr, ldo;
+  int m, n, k, act;
+};
+hipError_t launch_linear_q8(int dtype, const LinearQ8Args& a, hipStream_t s);
+
+// Normalisation into 8-bit codes (dare_k_norm_q8)
+struct NormQ8Args {
+  const void* x;
+  const void* o;      // or nullptr
+  void* x_out;        // or nullptr
+  const void* gain;
+  const void* bias;
+  int8_t* codes;
+  float* scales;
+  long ldx, ldo, ldxo, ldc;
+  double eps;
+  int kind, rows, d;
+};
+hipError_t launch_norm_q8(int dtype, const NormQ8Args& a, hipStream_t s);
+
+// Log-probabilities, entropy and alternatives of logits (dare_k_logprobs)
+struct LogprobsArgs {
+  const void* logits;
+  long ld;
+  int rows, vocab, top;
+  float scale;
+  const int32_t* tokens;   // with logprobs, or nullptr
+  float* logprobs;
+  float* entropy;          // or nullptr
+  int32_t* top_ids;        // [rows, top]
+  float* top_logprobs;
+};
+constexpr int kTopMost = 32;
+hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s);
 
 struct RopeArgs {
   const void* x[3];  // q, k, v or nullptr

@@ -617,7 +617,6 @@ __global__ void __launch_bounds__(512) linear_bf16_skinny_kernel(GemmDev p) {
 // return at once, costs 1 us more at 205 rows); the shape is the one that best_tile (gemm_route.h) names, and
 // its tiles are walked in passes.
 constexpr int kWideSmem = pp_smem_bytes<2>();
-constexpr int kWideGrid = 256;  // workgroups of a launch: one per CU
 // The refreshed-row list from the mask bytes, by every workgroup for itself (Alg. 1/2 line 5
 // folded into the first kernel that needs the list: a compaction kernel of its own costs a
 // launch, 4-5 us of a 90 us step, for a few hundred bytes of work).  512 threads, up to
@@ -1095,8 +1094,6 @@ GemmDev to_dev(const GemmArgs& g) {
   p.part_m_dev = g.part_m_dev;
   return p;
 }
-
-int grid_for(int tiles) { return ((tiles + 7) / 8) * 8; }
 
 // Outputs larger than half of the last-level cache (256 MB) are stored past the L2: what the stages behind them read first is
 // no longer there anyway, and the operands stay in its place (us, stored through the L2 and past it, in a step of 8 x 2048 tokens of hidden 4096:

@@ -53,14 +53,6 @@ struct GemmF32Dev {
   };
 };
 
-// silu(z) = z / (1 + e^-z); gelu(z) = z Phi(z) = z erfc(-z / sqrt(2)) / 2; its tanh form z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
-// Of -infinity gelu is 0, as in bf16; the others are the quotient of two infinities there.
-__device__ __forceinline__ float activate_f32(int act, float z) {
-  if (act == DARE_ACT_SILU) return z / (1.f + expf(-z));
-  if (act == DARE_ACT_GELU) return 0.5f * (z == -INFINITY ? -__FLT_MAX__ : z) * erfcf(-0.70710678f * z);  // (next to a 0)
-  if (act == DARE_ACT_GELU_TANH) return z / (1.f + expf(-1.59576912f * fmaf(0.044715f * z * z, z, z)));
-  return z;
-}
 __device__ __forceinline__ void store4_linear_f32(const GemmF32Dev& p, long tok, int col, f32x4 v) {
   if (p.bias) v += *reinterpret_cast<const f32x4*>(p.bias + col);
 #pragma unroll

@@ -178,6 +178,16 @@ constexpr GemmRoute linear_route(int m, int n, int k) {
   return gemm_route(m, n, k, 1, false);
 }
 
+// 8-bit codes: the shapes of linear_route for the same bytes of k (k in units of two codes).  The wide tiles are the four-wave ones, where they can
+// run (bf16 outputs, three k-steps); 128 x 192 stands for the others.
+constexpr GemmRoute linear_q8_route(int m, int n, int k, bool bf16) {
+  const GemmRoute r = linear_route(m, n, k);
+  const bool quad = bf16 && k / kRouteBK >= kQuadMinSteps;
+  if (r == GemmRoute::kPp192 || r == GemmRoute::kQuad192) return quad ? GemmRoute::kQuad192 : GemmRoute::k128x192;
+  if (r == GemmRoute::kPp256 || r == GemmRoute::kQuad256) return quad ? GemmRoute::kQuad256 : GemmRoute::k128x192;
+  return r == GemmRoute::kPp128 ? GemmRoute::k128x128 : r;
+}
+
 // What a launch of `tiles` tiles takes where it is compared with one of another number of tiles: rounds of the CUs above all, idle CUs
 // in a round save a quarter of their share.  `full` as in tile_cost.
 constexpr long rounds_cost(long tiles, int full) { return full * ((tiles + 255) / 256 * 768 + tiles) / 2; }

@@ -607,7 +607,7 @@ __device__ __forceinline__ void gemm_tiles_quad(const typename Op::Dev& p, const
       const int row = m0 + (wave * AL + i) * 8 + (lane >> 3);
       row_in[i] = row < rows_end ? row : rows_end - 1;
     }
-    row_tokens(list, nullptr, row_in, tok_in);
+    row_tokens(Op::kScaled ? nullptr : list, nullptr, row_in, tok_in);
   };
   const bf16_t* src_a[AL];
   const bf16_t* src_b[BL];
@@ -738,7 +738,7 @@ __device__ __forceinline__ void gemm_tiles_quad(const typename Op::Dev& p, const
       live[i] = row < rows_end;
       row_out[i] = row < rows_end ? row : rows_end - 1;
     }
-    row_tokens(list, nullptr, row_out, tok);
+    row_tokens(Op::kScaled ? nullptr : list, nullptr, row_out, tok);
     const int col0 = n0 + wn * (32 * TN), n_end = cols_end;
     vb += gridDim.x;
     const bool more = place();
@@ -759,13 +759,85 @@ __device__ __forceinline__ void gemm_tiles_quad(const typename Op::Dev& p, const
     // (what the compiler would know of MFMAs of its own: their results are there 18 cycles later)
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
     auto value = [&](int i, int j, int e) __attribute__((always_inline)) {
-      float v;
+      std::conditional_t<Op::kScaled, int, float> v;
       asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j * 2 + (e >> 2)][e & 3]));
-      return v;
+      return (float)v;
     };
     // acc[i][2 j + h][e] = C[row, col], row = m0 + 128 wm + 16 i + l16, col = col0 + 32 j + 8 kq + 4 h + e
     const bool low = l16 < 8;
-    if (!PART && !LINEAR && p.swiglu_pairs) {
+    if constexpr (Op::kScaled) {
+      float row_scale[NA];
+#pragma unroll
+      for (int i = 0; i < NA; ++i) row_scale[i] = p.row_scale[tok[i]];
+      // Two column blocks after the other, each with all rows: what belongs to a column (scale, bias) is held for two blocks and not
+      // for all, which would be 74 registers more than there are.  The rows' scales and residuals a row of the tile ahead.
+      const long ldc = p.ldc;
+#pragma unroll
+      for (int j = 0; j < TN; j += 2) {
+        constexpr int H = 2;
+        f32x4 col_scale[H][2];
+        bf16x8 bias[H], res[2][H];
+        int at_col[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+          if (j + h < TN) {
+            const int c = col0 + (j + h) * 32 + kq * 8;
+            at_col[h] = c < n_end ? c : n_end - 8;  // (columns behind the last one read the last ones, nobody stores them)
+            const f32x4* scale = reinterpret_cast<const f32x4*>(p.col_scale + at_col[h]);
+            col_scale[h][0] = scale[0];
+            col_scale[h][1] = scale[1];
+            bias[h] = p.bias ? *reinterpret_cast<const bf16x8*>(p.bias + at_col[h]) : bf16x8{};
+          }
+        auto ahead = [&](int i) __attribute__((always_inline)) {
+          const bf16_t* row = p.residual + tok[i] * p.ldr;
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+            if (j + h < TN) res[i & 1][h] = *reinterpret_cast<const bf16x8*>(row + at_col[h]);
+        };
+        if (p.residual) ahead(0);
+        const bool pair = j + 1 < TN;
+        const int c = col0 + j * 32 + (pair && !low ? 32 : 0);
+        bf16_t* to = c >= n_end ? nullptr : p.c0 + c + kq * 8;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+          const int other = from_half_row<0xf>(0, tok[i]);
+          const bool live_other = from_half_row<0xf>(0, live[i]) != 0;
+          const long own = tok[i] * ldc, far = other * ldc;
+          if (p.residual && i + 1 < NA) ahead(i + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 o[H];
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+            if (j + h < TN) {
+              float v[8];
+              bf16x8 r;
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                v[e] = fmaf(value(i, j + h, e) * row_scale[i], col_scale[h][e >> 2][e & 3], (float)bias[h][e]);
+              activate(p.act, v);
+              if (p.residual) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += (float)res[i & 1][h][e];
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e) r[e] = (bf16_t)v[e];
+              o[h] = __builtin_bit_cast(u32x4, r);
+            }
+          if (pair) {
+            u32x4 x, y;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              x[q] = from_half_row<0xc>(o[0][q], o[1][q]);
+              y[q] = from_half_row<0x3>(o[1][q], o[0][q]);
+            }
+            if (to && (low ? live[i] : live_other)) store16<STREAM>(to + (low ? own : far), x);
+            if (to && (low ? live_other : live[i])) store16<STREAM>(to + (low ? far : own), y);
+          } else if (to && live[i]) {
+            store16<STREAM>(to + own, o[0]);
+          }
+        }
+      }
+    } else if (!PART && !LINEAR && p.swiglu_pairs) {
       const long ldc = p.ldc;
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
@@ -1001,22 +1073,16 @@ __device__ __forceinline__ void skinny_tile(const typename Op::Dev& p, const int
       for (int u = 0; u < UNR; ++u) {
         const bool live = s + u < s1;
         if (LINEAR && !live) {  // (nothing is loaded, and no infinity meets a zero)
+          wf[u] = Frag{};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            wf[u][e] = (bf16_t)0.0f;
-#pragma unroll
-            for (int t = 0; t < TMS; ++t) xf[t][u][e] = (bf16_t)0.0f;
-          }
+          for (int t = 0; t < TMS; ++t) xf[t][u] = Frag{};
           continue;
         }
         const int ks = (live ? s + u : s0) << 5;
         wf[u] = *reinterpret_cast<const Frag*>(wrow + ks);
 #pragma unroll
         for (int t = 0; t < TMS; ++t) xf[t][u] = *reinterpret_cast<const Frag*>(xrow[t] + ks);
-        if (!live) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) wf[u][e] = (bf16_t)0.0f;
-        }
+        if (!live) wf[u] = Frag{};
       }
 #pragma unroll
       for (int u = 0; u < UNR; ++u)
@@ -1050,6 +1116,9 @@ __device__ __forceinline__ void skinny_tile(const typename Op::Dev& p, const int
   }
 }
 constexpr int kSkinnyRows = 32;
+
+constexpr int kWideGrid = 256;  // workgroups of a launch that walks over its tiles: one per CU
+int grid_for(int tiles) { return ((tiles + 7) / 8) * 8; }
 
 }  // namespace
 }  // namespace dare

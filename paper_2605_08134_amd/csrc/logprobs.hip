@@ -1,0 +1,304 @@
+// Log-probabilities of given tokens, entropy and top alternatives of rows of logits x, z = scale x:
+//     m = max x,  S = sum exp(scale (x - m)),  logprob(v) = scale (x_v - m) - log S,
+//     entropy = log S + sum exp(scale (x - m)) scale (m - x) / S
+//
+// One workgroup per row and one pass over it, bound by memory (exponentials: 64 elements take a SIMD 45 cycles, which is 7 TB/s for bf16).
+// Every lane keeps the sums over its elements relative to its own maximum; they are joined at the end.
+//
+// Alternatives.  Order: the larger logit first, of equal ones the lower id; as whole numbers, `order_key`, in which no two elements are equal.
+// In the pass a lane keeps only its largest chunk (16 bytes) and where that lies.  Take T, the k-th largest of the lanes' keys, or a lower one:
+// an element below T has k better ones, so the alternatives lie in the lanes whose key is T or more, about k of them; those lanes' elements are
+// read again (k / 1024 of the row), the ones from T on are listed, and a listed element's rank is how many others are above it.
+// The list may overflow where many of the largest logits fall into the same few lanes; then the alternatives are found one after the other.
+#include "dare_common.h"
+
+namespace dare {
+namespace {
+
+typedef unsigned long long u64;
+
+template <typename T>
+struct LogprobsDev {
+  const T* x;
+  long ld;
+  int vocab, top;
+  float scale;
+  const int32_t* tokens;
+  float* logprobs;
+  float* entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+};
+
+constexpr int kListed = 2048;   // elements that the list holds
+constexpr int kAhead = 4;       // chunks of a lane in flight
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// Elements of 16 bytes
+__device__ __forceinline__ void unpack(const bf16_t*, const u32x4 r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? r[e >> 1] & 0xffff0000u : r[e >> 1] << 16);
+}
+__device__ __forceinline__ void unpack(const float*, const u32x4 r, float (&v)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(r[e]);
+}
+
+// (value, place): larger values first, then lower places; 0 is below all.  Both zeros are one value.
+__device__ __forceinline__ u64 order_key(float v, unsigned place) {
+  const unsigned b = __float_as_uint(v + 0.f);
+  return (u64)(b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u)) << 32 | (unsigned)~place;
+}
+__device__ __forceinline__ float key_value(u64 key) {
+  const unsigned b = (unsigned)(key >> 32);
+  return __uint_as_float(b ^ ((int)b < 0 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ u64 wave_max(u64 v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const u64 w = __shfl_xor(v, o, 64);
+    v = w > v ? w : v;
+  }
+  return v;
+}
+
+// Sums relative to a maximum, in units of 2^(c (x - m)), c = scale log2(e)
+struct Sums {
+  float m;  // -FLT_MAX without an element
+  float s;  // sum of exponentials
+  float t;  // sum of exponential * c (x - m), at most 0
+};
+// What a sum and its moment become when their maximum rises to m
+__device__ __forceinline__ void raise(Sums& a, float m, float c) {
+  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+  a.t = f * fmaf(fmaxf(d, -200.f), a.s, a.t);
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Sums shuffled(Sums a, int o) {
+  return {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)};
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  raise(a, m, c);
+  raise(b, m, c);
+  return {m, a.s + b.s, a.t + b.t};
+}
+
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) {
+  constexpr int WAVES = THREADS / 64, E = 16 / sizeof(T);
+  // a wave's largest keys: enough for the k-th largest, and so many that it is near it
+  constexpr int MOST = 32 / WAVES > 4 ? 32 / WAVES : 4;
+  __shared__ Sums wave_sums[WAVES];
+  __shared__ u64 wave_keys[WAVES * MOST], listed[kListed], limit;
+  __shared__ int lanes[THREADS], n_lanes, n_listed;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long row = blockIdx.x;
+  const T* x = p.x + row * p.ld;
+  const float c = p.scale * kLog2e;
+  // elements in front of the first 16-byte boundary, whole chunks, elements behind the last one
+  const int to_boundary = (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T);
+  const int head = to_boundary < p.vocab ? to_boundary : p.vocab;
+  const int chunks = (p.vocab - head) / E, singles = p.vocab - chunks * E;
+  const T* body = x + head;
+  auto single_place = [&](int i) { return i < head ? i : i + chunks * E; };
+  auto chunk = [&](int i) { return reinterpret_cast<const u32x4*>(body)[i]; };
+  if (tid == 0) n_lanes = n_listed = 0;
+
+  float best = -INFINITY;  // largest element, and the first place of its chunk
+  unsigned place = 0;
+  Sums sum = {-__FLT_MAX__, 0.f, 0.f};
+  auto take = [&](const float (&v)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float d = (v[e] - sum.m) * c, f = __builtin_amdgcn_exp2f(d);
+      sum.s += f;
+      sum.t = fmaf(f, fmaxf(d, -200.f), sum.t);  // (0 times infinity is none; a NaN stays in f)
+    }
+  };
+  for (int i = tid; i < chunks; i += kAhead * THREADS) {
+    u32x4 r[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      constexpr unsigned none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;  // -infinity
+      r[a] = u32x4{none, none, none, none};
+      if (i + a * THREADS < chunks) r[a] = chunk(i + a * THREADS);
+    }
+    float v[kAhead][E], m = sum.m;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      unpack(x, r[a], v[a]);
+      float cm = v[a][0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) cm = fmaxf(cm, v[a][e]);
+      if (cm > best) {
+        best = cm;
+        place = head + (i + a * THREADS) * E;
+      }
+      m = fmaxf(m, cm);
+    }
+    raise(sum, m, c);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) take(v[a]);
+  }
+  if (tid < singles) {
+    const unsigned at = single_place(tid);
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = -INFINITY;
+    v[0] = (float)x[at];
+    if (v[0] > best || (v[0] == best && v[0] > -INFINITY && at < place)) {
+      best = v[0];
+      place = at;
+    }
+    raise(sum, fmaxf(sum.m, v[0]), c);
+    take(v);
+  }
+
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum = join(sum, shuffled(sum, o), c);
+  if (lane == 0) wave_sums[wave] = sum;
+  const int top = p.top;
+  u64 key = best > -INFINITY ? order_key(best, place) : 0;
+  if (top > 0) {
+    const int most = (top + WAVES - 1) / WAVES > 4 ? (top + WAVES - 1) / WAVES : top < 4 ? top : 4;
+    u64 k = key;
+    for (int j = 0; j < most; ++j) {
+      const u64 w = wave_max(k);
+      if (k == w) k = 0;  // (keys differ, but for 0)
+      if (lane == 0) wave_keys[wave * most + j] = w;
+    }
+    __syncthreads();
+    if (wave == 0) {  // the one with top - 1 keys above it; without so many keys: 1, which is below all
+      const int n = WAVES * most;
+      const u64 own = lane < n ? wave_keys[lane] : 0;
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += wave_keys[j] > own;
+      if (lane == 0) limit = 1;
+      if (own > 0 && above == top - 1) limit = own;
+    }
+  }
+  __syncthreads();
+  Sums all = wave_sums[lane % WAVES];
+#pragma unroll
+  for (int o = WAVES / 2; o > 0; o >>= 1) all = join(all, shuffled(all, o), c);
+  // (a NaN, or the difference of two infinities, is in the sum)
+  const bool undefined = !(all.s >= 0.f), empty = all.s == 0.f;
+  const float log_sum = logf(all.s);
+  auto logprob = [&](float v) {
+    return undefined ? __builtin_nanf("") : v == -INFINITY ? -INFINITY : (v - all.m) * p.scale - log_sum;
+  };
+  if (tid == 0) {
+    if (p.tokens) {
+      const int token = p.tokens[row];
+      p.logprobs[row] = logprob(token >= 0 && token < p.vocab ? (float)x[token] : -INFINITY);
+    }
+    if (p.entropy) p.entropy[row] = undefined ? __builtin_nanf("") : empty ? 0.f : fmaxf(log_sum - kLn2 * all.t / all.s, 0.f);
+  }
+  if (top == 0) return;
+
+  int32_t* ids = p.top_ids + row * top;
+  float* tops = p.top_logprobs + row * top;
+  if (undefined) {
+    if (tid < top) {
+      ids[tid] = -1;
+      tops[tid] = __builtin_nanf("");
+    }
+    return;
+  }
+  const u64 from = limit;
+  if (key >= from) lanes[atomicAdd(&n_lanes, 1)] = tid;
+  __syncthreads();
+  // the elements of the listed lanes: chunks l, l + THREADS, .. of each lane, then its single one
+  const int per_lane = (chunks + THREADS - 1) / THREADS + 1, n = n_lanes * per_lane;
+  auto elements = [&](auto use) {
+    for (int i = tid; i < n; i += THREADS) {
+      const int l = lanes[i / per_lane], j = i % per_lane;
+      if (j < per_lane - 1) {
+        const int at = l + j * THREADS;
+        if (at >= chunks) continue;
+        float v[E];
+        unpack(x, chunk(at), v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) use(v[e], head + at * E, e);
+      } else if (l < singles) {
+        use((float)x[single_place(l)], single_place(l), 0);
+      }
+    }
+  };
+  // (the limit is a lane's key: its value with the first place of its chunk)
+  elements([&](float v, int first, int e) {
+    if (v > -INFINITY && order_key(v, first) >= from) {
+      const int at = atomicAdd(&n_listed, 1);
+      if (at < kListed) listed[at] = order_key(v, first + e);
+    }
+  });
+  __syncthreads();
+  const int found = n_listed;
+  if (found <= kListed) {
+    for (int i = tid; i < found; i += THREADS) {
+      const u64 own = listed[i];
+      int above = 0;
+      for (int j = 0; j < found; ++j) above += listed[j] > own;
+      if (above < top) {
+        ids[above] = (int32_t)~(unsigned)own;
+        tops[above] = logprob(key_value(own));
+      }
+    }
+    if (tid >= found && tid < top) {
+      ids[tid] = -1;
+      tops[tid] = -INFINITY;
+    }
+    return;
+  }
+  // more than the list holds: one after the other (there are more than `top`)
+  u64 last = ~0ull;
+  for (int k = 0; k < top; ++k) {
+    u64 next = 0;
+    elements([&](float v, int first, int e) {
+      const u64 own = v > -INFINITY ? order_key(v, first + e) : 0;
+      if (own < last && own > next) next = own;
+    });
+    next = wave_max(next);
+    __syncthreads();
+    if (lane == 0) wave_keys[wave] = next;
+    __syncthreads();
+    next = wave_max(wave_keys[lane % WAVES]);
+    last = next;
+    if (tid == 0) {
+      ids[k] = (int32_t)~(unsigned)last;
+      tops[k] = logprob(key_value(last));
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch(const LogprobsArgs& a, hipStream_t s) {
+  LogprobsDev<T> p;
+  p.x = static_cast<const T*>(a.logits);
+  p.ld = a.ld;
+  p.vocab = a.vocab;
+  p.top = a.top;
+  p.scale = a.scale;
+  p.tokens = a.tokens;
+  p.logprobs = a.logprobs;
+  p.entropy = a.entropy;
+  p.top_ids = a.top_ids;
+  p.top_logprobs = a.top_logprobs;
+  if (a.vocab < 16384)
+    hipLaunchKernelGGL((logprobs_kernel<T, 256>), dim3(a.rows), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((logprobs_kernel<T, 1024>), dim3(a.rows), dim3(1024), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  return dtype == DARE_BF16 ? launch<bf16_t>(a, s) : launch<float>(a, s);
+}
+
+}  // namespace dare

@@ -1,0 +1,345 @@
+// Normalisation of token rows into 8-bit codes with a scale per row, with the residual sum in front of it:
+//     s = x + o, rounded to the type and stored;   y = s | LayerNorm(s) | s / sqrt(mean(s^2) + eps) * gain
+//     scale = max |y| / 127 rounded to fp32;       code = y / scale to the nearest whole number, ties to even
+//
+// Everything behind s is formed in 64 bits: a code is the one that the formula has.  In fp32 y / scale is off by up to 127 * 4 * 2^-24 =
+// 3e-5, and a row's codes would hang on the order in which its sum of squares was formed: one code in 10^5 goes to a neighbour, and
+// no other program could say which.
+//
+// Memory-bound: one read of x and o, one write of s and of a byte per channel.  A row is held in registers, as 64-bit values, from its
+// load to its codes, by a wave (rows of up to 2048 channels) or a workgroup of four waves (up to 16384); longer rows are read once per
+// pass.
+#include "dare_common.h"
+
+namespace dare {
+namespace {
+
+template <typename T>
+struct NormQ8Dev {
+  const T* x;
+  const T* o;       // or nullptr
+  T* x_out;         // or nullptr
+  const T* gain;    // nullptr: none
+  const T* bias;    // LayerNorm
+  int8_t* codes;
+  float* scales;
+  long ldx, ldo, ldxo, ldc;
+  double eps;
+  int rows, d;
+};
+
+// 8 neighbouring channels
+struct Raw8 {
+  u32x4 w[2];
+};
+__device__ __forceinline__ void load8(const bf16_t* p, Raw8& r) { r.w[0] = *reinterpret_cast<const u32x4*>(p); }
+__device__ __forceinline__ void load8(const float* p, Raw8& r) {
+  r.w[0] = reinterpret_cast<const u32x4*>(p)[0];
+  r.w[1] = reinterpret_cast<const u32x4*>(p)[1];
+}
+__device__ __forceinline__ void values8(const bf16_t*, const Raw8& r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? r.w[0][e >> 1] & 0xffff0000u : r.w[0][e >> 1] << 16);
+}
+__device__ __forceinline__ void values8(const float*, const Raw8& r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r.w[e >> 2][e & 3]);
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+  bf16x8 t;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = (bf16_t)v[e];
+  *reinterpret_cast<bf16x8*>(p) = t;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) reinterpret_cast<f32x4*>(p)[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+}
+
+__device__ __forceinline__ double add2(double a, double b) { return a + b; }
+__device__ __forceinline__ double max2(double a, double b) { return fmax(a, b); }
+// Over the lanes of a row: a wave's, or, with four waves, the workgroup's through LDS (`sh`: 4 values that nothing else uses)
+template <int WAVES, class F>
+__device__ __forceinline__ double reduce(double v, F f, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v = f(v, sh[w]);
+  }
+  return v;
+}
+
+// The code of y: its quotient by the scale (y / scale rounded once, by a product and a correction), to the nearest whole number by
+// adding 1.5 * 2^52, which leaves it in the low bits.
+__device__ __forceinline__ int code_of(double y, double scale, double inverse) {
+  double q = y * inverse;
+  q = fma(fma(-q, scale, y), inverse, q);
+  const int c = __double2loint(q + 6755399441055744.0);
+  return min(max(c, -127), 127);  // (a scale that is no normal number may be off by half)
+}
+__device__ __forceinline__ u32x2 pack8(const int (&c)[8]) {
+  u32x2 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    r[h] = (unsigned)(c[4 * h] & 255) | (unsigned)(c[4 * h + 1] & 255) << 8 | (unsigned)(c[4 * h + 2] & 255) << 16 | (unsigned)c[4 * h + 3] << 24;
+  return r;
+}
+
+struct RowScale {
+  double scale, inverse;
+  bool finite;
+};
+// largest: max |y|; rest: 0, or NaN where some y is not finite
+__device__ __forceinline__ RowScale row_scale(double largest, double rest, float* to, bool writes) {
+  RowScale r;
+  r.finite = rest == 0.0;
+  const float scale = r.finite ? (float)(largest / 127.0) : __builtin_nanf("");
+  r.scale = scale;
+  r.inverse = scale > 0.f ? 1.0 / r.scale : 0.0;
+  if (writes) *to = scale;
+  return r;
+}
+
+// Rows of up to WAVES * 512 HOLD channels, 4 / WAVES of them per workgroup
+template <typename T, int KIND, int WAVES, int HOLD>
+__global__ void __launch_bounds__(256) norm_q8_kernel(NormQ8Dev<T> p) {
+  constexpr int LANES = WAVES * 64, ROWS = 4 / WAVES;
+  __shared__ double sh[4][4];
+  const int lane = threadIdx.x % LANES;
+  const long row = (long)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (row >= p.rows) return;  // (whole waves; with four waves per row no workgroup)
+  const T* x = p.x + row * p.ldx;
+  const T* o = p.o + row * p.ldo;
+  const int groups = p.d >> 3;
+  double y[HOLD][8];
+  {
+    Raw8 a[HOLD], b[HOLD];
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+      const int g = lane + h * LANES;
+      a[h] = b[h] = Raw8{};
+      if (g < groups) {
+        load8(x + g * 8, a[h]);
+        if (p.o) load8(o + g * 8, b[h]);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+      const int g = lane + h * LANES;
+      float v[8], w[8];
+      values8(x, a[h], v);
+      if (p.o) {
+        values8(o, b[h], w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)(T)(v[e] + w[e]);
+      }
+      if (p.x_out && g < groups) store8(p.x_out + row * p.ldxo + g * 8, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[h][e] = v[e];
+    }
+  }
+  if constexpr (KIND != DARE_NORM_NONE) {
+    double mean = 0.0, sum = 0.0;
+    if constexpr (KIND == DARE_NORM_LAYER) {
+#pragma unroll
+      for (int h = 0; h < HOLD; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += y[h][e];
+      mean = reduce<WAVES>(sum, add2, sh[0]) / p.d;
+      sum = 0.0;
+    }
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (KIND == DARE_NORM_LAYER) y[h][e] = lane + h * LANES < groups ? y[h][e] - mean : 0.0;
+        sum = fma(y[h][e], y[h][e], sum);
+      }
+    const double r = 1.0 / sqrt(reduce<WAVES>(sum, add2, sh[1]) / p.d + p.eps);
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h) {
+      const int g = lane + h * LANES;
+      if (g < groups) {
+        Raw8 t;
+        float v[8];
+        load8(p.gain + g * 8, t);
+        values8(x, t, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[h][e] *= r * v[e];
+        if constexpr (KIND == DARE_NORM_LAYER) {
+          if (p.bias) {
+            load8(p.bias + g * 8, t);
+            values8(x, t, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[h][e] += v[e];
+          }
+        }
+      }
+    }
+  }
+  double largest = 0.0, rest = 0.0;  // rest: a NaN that stays if some value is not finite
+#pragma unroll
+  for (int h = 0; h < HOLD; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      largest = fmax(largest, fabs(y[h][e]));
+      rest = fma(y[h][e], 0.0, rest);
+    }
+  largest = reduce<WAVES>(largest, max2, sh[2]);
+  rest = reduce<WAVES>(rest, add2, sh[3]);
+  const RowScale s = row_scale(largest, rest, p.scales + row, lane == 0);
+#pragma unroll
+  for (int h = 0; h < HOLD; ++h) {
+    const int g = lane + h * LANES;
+    int c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = s.finite ? code_of(y[h][e], s.scale, s.inverse) : 0;
+    if (g < groups) *reinterpret_cast<u32x2*>(p.codes + row * p.ldc + g * 8) = pack8(c);
+  }
+}
+
+// Rows of any length, a workgroup each, read once for every sum, for the largest value and for the codes
+template <typename T, int KIND>
+__global__ void __launch_bounds__(256) norm_q8_long_kernel(NormQ8Dev<T> p) {
+  __shared__ double sh[4][4];
+  const long row = blockIdx.x;
+  const T* x = p.x + row * p.ldx;
+  const T* o = p.o ? p.o + row * p.ldo : nullptr;
+  T* x_out = p.x_out ? p.x_out + row * p.ldxo : nullptr;
+  const int groups = p.d >> 3;
+  bool summed = false;  // x_out holds the sum (and may be x)
+  auto sum_of = [&](int g, double (&y)[8]) {
+    Raw8 t;
+    float v[8], w[8];
+    if (summed) {
+      load8(x_out + g * 8, t);
+      values8(x, t, v);
+    } else {
+      load8(x + g * 8, t);
+      values8(x, t, v);
+      if (o) {
+        load8(o + g * 8, t);
+        values8(x, t, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)(T)(v[e] + w[e]);
+      }
+      if (x_out) store8(x_out + g * 8, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = v[e];
+  };
+  double mean = 0.0, r = 1.0, y[8];
+  if constexpr (KIND == DARE_NORM_LAYER) {
+    double sum = 0.0;
+    for (int g = threadIdx.x; g < groups; g += 256) {
+      sum_of(g, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += y[e];
+    }
+    summed = x_out != nullptr;
+    mean = reduce<4>(sum, add2, sh[0]) / p.d;
+  }
+  if constexpr (KIND != DARE_NORM_NONE) {
+    double sum = 0.0;
+    for (int g = threadIdx.x; g < groups; g += 256) {
+      sum_of(g, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma(y[e] - mean, y[e] - mean, sum);
+    }
+    summed = x_out != nullptr;
+    r = 1.0 / sqrt(reduce<4>(sum, add2, sh[1]) / p.d + p.eps);
+  }
+  auto value = [&](int g, double (&y)[8]) {
+    sum_of(g, y);
+    if constexpr (KIND != DARE_NORM_NONE) {
+      Raw8 t;
+      float v[8];
+      load8(p.gain + g * 8, t);
+      values8(x, t, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = (y[e] - mean) * (r * v[e]);
+      if (p.bias) {
+        load8(p.bias + g * 8, t);
+        values8(x, t, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += v[e];
+      }
+    }
+  };
+  double largest = 0.0, rest = 0.0;
+  for (int g = threadIdx.x; g < groups; g += 256) {
+    value(g, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      largest = fmax(largest, fabs(y[e]));
+      rest = fma(y[e], 0.0, rest);
+    }
+  }
+  summed = x_out != nullptr;
+  largest = reduce<4>(largest, max2, sh[2]);
+  rest = reduce<4>(rest, add2, sh[3]);
+  const RowScale s = row_scale(largest, rest, p.scales + row, threadIdx.x == 0);
+  for (int g = threadIdx.x; g < groups; g += 256) {
+    value(g, y);
+    int c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = s.finite ? code_of(y[e], s.scale, s.inverse) : 0;
+    *reinterpret_cast<u32x2*>(p.codes + row * p.ldc + g * 8) = pack8(c);
+  }
+}
+
+template <typename T, int KIND>
+hipError_t launch(const NormQ8Dev<T>& p, hipStream_t s) {
+  const int rows4 = (p.rows + 3) / 4;
+  if (p.d <= 512)
+    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 1, 1>), dim3(rows4), dim3(256), 0, s, p);
+  else if (p.d <= 2048)
+    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 1>), dim3(p.rows), dim3(256), 0, s, p);
+  else if (p.d <= 4096)
+    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 2>), dim3(p.rows), dim3(256), 0, s, p);
+  else if (p.d <= 8192)
+    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 4>), dim3(p.rows), dim3(256), 0, s, p);
+  else if (p.d <= 16384)
+    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 8>), dim3(p.rows), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((norm_q8_long_kernel<T, KIND>), dim3(p.rows), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const NormQ8Args& a, hipStream_t s) {
+  NormQ8Dev<T> p;
+  p.x = static_cast<const T*>(a.x);
+  p.o = static_cast<const T*>(a.o);
+  p.x_out = static_cast<T*>(a.x_out);
+  p.gain = static_cast<const T*>(a.gain);
+  p.bias = static_cast<const T*>(a.bias);
+  p.codes = a.codes;
+  p.scales = a.scales;
+  p.ldx = a.ldx;
+  p.ldo = a.ldo;
+  p.ldxo = a.ldxo;
+  p.ldc = a.ldc;
+  p.eps = a.eps;
+  p.rows = a.rows;
+  p.d = a.d;
+  switch (a.kind) {
+    case DARE_NORM_NONE: return launch<T, DARE_NORM_NONE>(p, s);
+    case DARE_NORM_LAYER: return launch<T, DARE_NORM_LAYER>(p, s);
+    case DARE_NORM_RMS: return launch<T, DARE_NORM_RMS>(p, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_norm_q8(int dtype, const NormQ8Args& a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  return dtype == DARE_BF16 ? launch_type<bf16_t>(a, s) : launch_type<float>(a, s);
+}
+
+}  // namespace dare
