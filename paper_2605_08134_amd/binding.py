@@ -798,9 +798,9 @@ def dare_k_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_ids=No
     top = 0 if top_ids is None else top_ids.shape[1]
     pi = pt = 0
     if top_ids is not None:
-        pi, ldi = _matrix("top_ids", top_ids, i32, device, rows, top)
-        pt, ldt = _matrix("top_logprobs", top_logprobs, f32, device, rows, top)
-        if ldi != top or ldt != top:
+        pi, _ = _matrix("top_ids", top_ids, i32, device, rows, top)
+        pt, _ = _matrix("top_logprobs", top_logprobs, f32, device, rows, top)
+        if not (top_ids.is_contiguous() and top_logprobs.is_contiguous()):
             raise ValueError("top_ids and top_logprobs must be contiguous")
     call = _pack(_LOGPROBS_CALL, code, rows, vocab, top, scale, ld, px, 0 if tokens is None else _vector("tokens", tokens, i32, device, rows),
                  0 if logprobs is None else _vector("logprobs", logprobs, f32, device, rows),

@@ -1,16 +1,18 @@
 // Log-probabilities of given tokens, entropy and top alternatives of rows of logits x, z = scale x:
-//     m = max x,  S = sum exp(scale (x - m)),  logprob(v) = scale (x_v - m) - log S,
-//     entropy = log S + sum exp(scale (x - m)) scale (m - x) / S
+//     S = sum exp(z - r),  logprob(v) = z_v - r - log S,  entropy = log S - sum exp(z - r) (z - r) / S,   r about max z
 //
 // One workgroup per row and one pass over it, bound by memory (exponentials: 64 elements take a SIMD 45 cycles, which is 7 TB/s for bf16).
-// Every lane keeps the sums over its elements relative to its own maximum; they are joined at the end.
+// Every lane keeps the sums over its elements relative to its own largest one; they are joined at the end.
 //
 // Alternatives.  Order: the larger logit first, of equal ones the lower id; as whole numbers, `order_key`, in which no two elements are equal.
 // In the pass a lane keeps only its largest chunk (16 bytes) and where that lies.  Take T, the k-th largest of the lanes' keys, or a lower one:
 // an element below T has k better ones, so the alternatives lie in the lanes whose key is T or more, about k of them; those lanes' elements are
 // read again (k / 1024 of the row), the ones from T on are listed, and a listed element's rank is how many others are above it.
 // The list may overflow where many of the largest logits fall into the same few lanes; then the alternatives are found one after the other.
+#include <type_traits>
+
 #include "dare_common.h"
+#include "lanes.h"
 
 namespace dare {
 namespace {
@@ -54,35 +56,35 @@ __device__ __forceinline__ float key_value(u64 key) {
   return __uint_as_float(b ^ ((int)b < 0 ? 0x80000000u : 0xffffffffu));
 }
 __device__ __forceinline__ u64 wave_max(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const u64 w = __shfl_xor(v, o, 64);
-    v = w > v ? w : v;
-  }
-  return v;
+  return over_lanes(v, [](u64 a, u64 b) { return a > b ? a : b; });
 }
 
-// Sums relative to a maximum, in units of 2^(c (x - m)), c = scale log2(e)
+// Sums of a set of elements in units of 2^r, exponents d = c x - r, c = scale log2(e), by one product and sum each.  r is near the largest of c x, and
+// any r is right: its rounding is in no exponent.  WIDE: r stands for an x and exponents are c (x - r), which takes an instruction more
+// and holds where c x does not (logits near the largest and lowest values of fp32).
 struct Sums {
-  float m;  // -FLT_MAX without an element
-  float s;  // sum of exponentials
-  float t;  // sum of exponential * c (x - m), at most 0
+  float r;  // -FLT_MAX without an element
+  float s;  // sum of 2^d
+  float t;  // sum of 2^d d
 };
-// What a sum and its moment become when their maximum rises to m
-__device__ __forceinline__ void raise(Sums& a, float m, float c) {
-  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
-  a.t = f * fmaf(fmaxf(d, -200.f), a.s, a.t);
+template <bool WIDE>
+__device__ __forceinline__ float exponent(float x, float r, float c) {
+  return WIDE ? (x - r) * c : fmaf(x, c, -r);
+}
+// The same sums in units of 2^r for a larger r
+template <bool WIDE>
+__device__ __forceinline__ void raise(Sums& a, float r, float c) {
+  const float d = WIDE ? (a.r - r) * c : a.r - r, f = __builtin_amdgcn_exp2f(d);
+  a.t = f * fmaf(fmaxf(d, -200.f), a.s, a.t);  // (0 times infinity is none; a NaN stays in the sum)
   a.s *= f;
-  a.m = m;
+  a.r = r;
 }
-__device__ __forceinline__ Sums shuffled(Sums a, int o) {
-  return {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)};
-}
+template <bool WIDE>
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  raise(a, m, c);
-  raise(b, m, c);
-  return {m, a.s + b.s, a.t + b.t};
+  const float r = fmaxf(a.r, b.r);
+  raise<WIDE>(a, r, c);
+  raise<WIDE>(b, r, c);
+  return {r, a.s + b.s, a.t + b.t};
 }
 
 template <typename T, int THREADS>
@@ -109,57 +111,63 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
 
   float best = -INFINITY;  // largest element, and the first place of its chunk
   unsigned place = 0;
-  Sums sum = {-__FLT_MAX__, 0.f, 0.f};
-  auto take = [&](const float (&v)[E]) {
+  // the row's sums, in wave_sums by waves
+  auto pass = [&](auto wide) {
+    constexpr bool WIDE = decltype(wide)::value;
+    Sums sum = {-__FLT_MAX__, 0.f, 0.f};
+    auto take = [&](const float (&v)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float d = (v[e] - sum.m) * c, f = __builtin_amdgcn_exp2f(d);
-      sum.s += f;
-      sum.t = fmaf(f, fmaxf(d, -200.f), sum.t);  // (0 times infinity is none; a NaN stays in f)
-    }
-  };
-  for (int i = tid; i < chunks; i += kAhead * THREADS) {
-    u32x4 r[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      constexpr unsigned none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;  // -infinity
-      r[a] = u32x4{none, none, none, none};
-      if (i + a * THREADS < chunks) r[a] = chunk(i + a * THREADS);
-    }
-    float v[kAhead][E], m = sum.m;
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      unpack(x, r[a], v[a]);
-      float cm = v[a][0];
-#pragma unroll
-      for (int e = 1; e < E; ++e) cm = fmaxf(cm, v[a][e]);
-      if (cm > best) {
-        best = cm;
-        place = head + (i + a * THREADS) * E;
+      for (int e = 0; e < E; ++e) {
+        const float d = exponent<WIDE>(v[e], sum.r, c), f = __builtin_amdgcn_exp2f(d);
+        sum.s += f;
+        sum.t = fmaf(f, fmaxf(d, -200.f), sum.t);
       }
-      m = fmaxf(m, cm);
+    };
+    auto rise = [&]() { raise<WIDE>(sum, fmaxf(sum.r, WIDE ? best : best * c), c); };
+    for (int i = tid; i < chunks; i += kAhead * THREADS) {
+      u32x4 r[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        constexpr unsigned none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;  // -infinity
+        r[a] = u32x4{none, none, none, none};
+        if (i + a * THREADS < chunks) r[a] = chunk(i + a * THREADS);
+      }
+      float v[kAhead][E];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        unpack(x, r[a], v[a]);
+        float most = v[a][0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) most = fmaxf(most, v[a][e]);
+        if (most > best) {
+          best = most;
+          place = head + (i + a * THREADS) * E;
+        }
+      }
+      rise();
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) take(v[a]);
     }
-    raise(sum, m, c);
+    if (tid < singles) {
+      const unsigned at = single_place(tid);
+      float v[E];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) take(v[a]);
-  }
-  if (tid < singles) {
-    const unsigned at = single_place(tid);
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = -INFINITY;
-    v[0] = (float)x[at];
-    if (v[0] > best || (v[0] == best && v[0] > -INFINITY && at < place)) {
-      best = v[0];
-      place = at;
+      for (int e = 0; e < E; ++e) v[e] = -INFINITY;
+      v[0] = (float)x[at];
+      if (v[0] > best || (v[0] == best && v[0] > -INFINITY && at < place)) {
+        best = v[0];
+        place = at;
+      }
+      rise();
+      take(v);
     }
-    raise(sum, fmaxf(sum.m, v[0]), c);
-    take(v);
-  }
-
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum = join(sum, shuffled(sum, o), c);
-  if (lane == 0) wave_sums[wave] = sum;
+    sum = over_lanes(sum, [&](Sums a, Sums b) { return join<WIDE>(a, b, c); });
+    if (lane == 0) wave_sums[wave] = sum;
+  };
+  auto joined = [&](auto wide) {
+    return over_lanes<0, WAVES == 16 ? 4 : 2>(wave_sums[lane % WAVES], [&](Sums a, Sums b) { return join<decltype(wide)::value>(a, b, c); });
+  };
+  pass(std::false_type{});
   const int top = p.top;
   u64 key = best > -INFINITY ? order_key(best, place) : 0;
   if (top > 0) {
@@ -175,27 +183,38 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
       const int n = WAVES * most;
       const u64 own = lane < n ? wave_keys[lane] : 0;
       int above = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) above += wave_keys[j] > own;
       if (lane == 0) limit = 1;
       if (own > 0 && above == top - 1) limit = own;
     }
   }
   __syncthreads();
-  Sums all = wave_sums[lane % WAVES];
-#pragma unroll
-  for (int o = WAVES / 2; o > 0; o >>= 1) all = join(all, shuffled(all, o), c);
+  Sums all = joined(std::false_type{});
+  // no sum: no element, one that is not finite, or a c x beyond fp32
+  const bool wide = !(all.s > 0.f);
+  if (wide) {
+    __syncthreads();
+    pass(std::true_type{});
+    __syncthreads();
+    all = joined(std::true_type{});
+  }
   // (a NaN, or the difference of two infinities, is in the sum)
   const bool undefined = !(all.s >= 0.f), empty = all.s == 0.f;
-  const float log_sum = logf(all.s);
+  const float log2_sum = __log2f(all.s);
   auto logprob = [&](float v) {
-    return undefined ? __builtin_nanf("") : v == -INFINITY ? -INFINITY : (v - all.m) * p.scale - log_sum;
+    if (undefined) return __builtin_nanf("");
+    if (v == -INFINITY) return -INFINITY;
+    if (wide) return (v - all.r) * p.scale - kLn2 * log2_sum;
+    const float d = fmaf(v, c, -all.r) - log2_sum;
+    return d > -INFINITY ? kLn2 * d : fmaf(v, p.scale, -kLn2 * all.r);  // (c v beyond fp32, scale v perhaps not)
   };
   if (tid == 0) {
     if (p.tokens) {
       const int token = p.tokens[row];
       p.logprobs[row] = logprob(token >= 0 && token < p.vocab ? (float)x[token] : -INFINITY);
     }
-    if (p.entropy) p.entropy[row] = undefined ? __builtin_nanf("") : empty ? 0.f : fmaxf(log_sum - kLn2 * all.t / all.s, 0.f);
+    if (p.entropy) p.entropy[row] = undefined ? __builtin_nanf("") : empty ? 0.f : fmaxf(kLn2 * (log2_sum - all.t / all.s), 0.f);
   }
   if (top == 0) return;
 
@@ -241,6 +260,7 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
     for (int i = tid; i < found; i += THREADS) {
       const u64 own = listed[i];
       int above = 0;
+#pragma unroll 8
       for (int j = 0; j < found; ++j) above += listed[j] > own;
       if (above < top) {
         ids[above] = (int32_t)~(unsigned)own;

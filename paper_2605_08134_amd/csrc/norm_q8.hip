@@ -10,6 +10,7 @@
 // load to its codes, by a wave (rows of up to 2048 channels) or a workgroup of four waves (up to 16384); longer rows are read once per
 // pass.
 #include "dare_common.h"
+#include "lanes.h"
 
 namespace dare {
 namespace {
@@ -61,8 +62,7 @@ __device__ __forceinline__ double max2(double a, double b) { return fmax(a, b); 
 // Over the lanes of a row: a wave's, or, with four waves, the workgroup's through LDS (`sh`: 4 values that nothing else uses)
 template <int WAVES, class F>
 __device__ __forceinline__ double reduce(double v, F f, double* sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
+  v = over_lanes(v, f);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();

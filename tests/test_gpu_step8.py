@@ -334,6 +334,10 @@ def test_logprobs_parts_that_are_left_out_and_no_rows():
     B.dare_k_logprobs(x, top_ids=part[2], top_logprobs=part[3])
     assert all(torch.equal(a, b) for a, b in zip(full, part))
     B.dare_k_logprobs(x)
+    B.dare_k_logprobs(x, tokens, part[0], part[1], part[2][:, :0].contiguous(), part[3][:, :0].contiguous())
+    assert torch.equal(full[0], part[0]) and torch.equal(full[1], part[1])
+    with pytest.raises(ValueError):
+        B.dare_k_logprobs(x, top_ids=part[2][:, :2], top_logprobs=part[3][:, :2])
     B.dare_k_logprobs(x[:0], tokens[:0], part[0][:0], part[1][:0], part[2][:0], part[3][:0])
 
 
