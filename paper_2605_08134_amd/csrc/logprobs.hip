@@ -79,12 +79,12 @@ __device__ __forceinline__ void raise(Sums& a, float r, float c) {
   a.s *= f;
   a.r = r;
 }
-template <bool WIDE>
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-  const float r = fmaxf(a.r, b.r);
-  raise<WIDE>(a, r, c);
-  raise<WIDE>(b, r, c);
-  return {r, a.s + b.s, a.t + b.t};
+// Of 2^TO lanes together
+template <bool WIDE, int TO = 6>
+__device__ __forceinline__ Sums join(Sums a, float c) {
+  raise<WIDE>(a, over_lanes<0, TO>(a.r, [](float x, float y) { return fmaxf(x, y); }), c);
+  const auto add = [](float x, float y) { return x + y; };
+  return {a.r, over_lanes<0, TO>(a.s, add), over_lanes<0, TO>(a.t, add)};
 }
 
 template <typename T, int THREADS>
@@ -161,21 +161,35 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
       rise();
       take(v);
     }
-    sum = over_lanes(sum, [&](Sums a, Sums b) { return join<WIDE>(a, b, c); });
+    sum = join<WIDE>(sum, c);
     if (lane == 0) wave_sums[wave] = sum;
   };
   auto joined = [&](auto wide) {
-    return over_lanes<0, WAVES == 16 ? 4 : 2>(wave_sums[lane % WAVES], [&](Sums a, Sums b) { return join<decltype(wide)::value>(a, b, c); });
+    return join<decltype(wide)::value, WAVES == 16 ? 4 : 2>(wave_sums[lane % WAVES], c);
   };
   pass(std::false_type{});
   const int top = p.top;
   u64 key = best > -INFINITY ? order_key(best, place) : 0;
   if (top > 0) {
     const int most = (top + WAVES - 1) / WAVES > 4 ? (top + WAVES - 1) / WAVES : top < 4 ? top : 4;
-    u64 k = key;
+    float left = best;  // of the lanes that are not taken yet
     for (int j = 0; j < most; ++j) {
-      const u64 w = wave_max(k);
-      if (k == w) k = 0;  // (keys differ, but for 0)
+      const float v = over_lanes(left, [](float a, float b) { return fmaxf(a, b); });
+      u64 equal = __ballot(left == v), w = 0;
+      if (v > -INFINITY) {
+        int owner = __ffsll((long long)equal) - 1;
+        unsigned first = __builtin_amdgcn_readlane(place, owner);
+        while (equal &= equal - 1) {  // the lowest place of equal ones
+          const int l = __ffsll((long long)equal) - 1;
+          const unsigned at = __builtin_amdgcn_readlane(place, l);
+          if (at < first) {
+            first = at;
+            owner = l;
+          }
+        }
+        w = order_key(v, first);
+        if (lane == owner) left = -INFINITY;
+      }
       if (lane == 0) wave_keys[wave * most + j] = w;
     }
     __syncthreads();
