@@ -325,9 +325,11 @@ dare_status dare_k_linear_q8(const dare_linear_q8_call* call, void* hip_stream);
  * Sums in fp32; a log-probability or an entropy is off by about 2^-22 of its size and of 1.
  *   logits [n_rows, ld] dtype, any alignment of an element; tokens [n_rows] int32 with logprobs [n_rows] fp32, or both NULL; entropy [n_rows]
  *   fp32 or NULL; top_ids [n_rows, top] int32, top_logprobs [n_rows, top] fp32
+ * workspace: dare_k_logprobs_workspace() bytes (for the same sizes; it does not look at the pointers), 16-byte aligned, needed while the call runs,
+ * not initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Nothing overlaps.  top is 0 .. 32 and at most vocab; scale (1 / temperature) above 0, at most 1e30.
  * Errors: INVALID_ARG (struct_size, null pointer, unknown dtype, sizes, scale, ld below vocab, alignment, tokens without logprobs or the other
- * way round), UNSUPPORTED (top above 32, n_rows beyond 2^21, vocab beyond 2^28, ld beyond 2^32).
+ * way round, workspace too small), UNSUPPORTED (top above 32, n_rows beyond 2^21, vocab beyond 2^28, ld beyond 2^32).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_logprobs_call) */
@@ -340,7 +342,8 @@ typedef struct {
   int32_t* top_ids;
   float* top_logprobs;
 } dare_logprobs_call;
-dare_status dare_k_logprobs(const dare_logprobs_call* call, void* hip_stream);
+dare_status dare_k_logprobs_workspace(const dare_logprobs_call* call, size_t* bytes);
+dare_status dare_k_logprobs(const dare_logprobs_call* call, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

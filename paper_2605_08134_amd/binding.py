@@ -31,7 +31,7 @@ EXPORTS = (
     "dare_model_set_prefix", "dare_model_step", "dare_model_logits", "dare_model_layer",
     "dare_model_destroy", "dare_model_last_error",
     "dare_k_linear", "dare_k_rope", "dare_k_rope_freqs", "dare_k_attention_packed", "dare_k_attention_packed_workspace",
-    "dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs",
+    "dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs", "dare_k_logprobs_workspace",
 )
 RULE_SCORE, RULE_QUANTILE = 0, 1
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
@@ -177,7 +177,11 @@ def lib():
     L.dare_k_quantile_mask.argtypes = [vp, i32, i32, f32, i32, vp, vp, vp, vp, vp]
     L.dare_k_quantile_mask.restype = i32
     lng = ctypes.c_long
-    for name in ("dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs"):
+    L.dare_k_logprobs.argtypes = [vp, vp, ctypes.c_size_t, vp]
+    L.dare_k_logprobs.restype = i32
+    L.dare_k_logprobs_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+    L.dare_k_logprobs_workspace.restype = i32
+    for name in ("dare_k_norm_q8", "dare_k_linear_q8"):
         getattr(L, name).argtypes = [vp, vp]
         getattr(L, name).restype = i32
     L.dare_k_linear.argtypes = [i32, vp, lng, vp, i32, i32, i32, vp, i32, vp, lng, vp, lng, vp]
@@ -784,10 +788,12 @@ def dare_k_linear_q8(a, a_scales, wt, wt_scales, out, bias=None, act=None, resid
     _enqueue(device, stream, lib().dare_k_linear_q8, call)
 
 
-def dare_k_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, scale=1.0, stream=None):
+def dare_k_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, scale=1.0,
+                    workspace=None, stream=None):
     """Of p = softmax(scale logits) per row of logits [rows, vocab]: logprobs = log p of tokens (int32 [rows]), the entropy, and ids and
     log-probabilities of the largest (top_ids int32, top_logprobs [rows, top], top up to 32; equal logits by their ids).  What is not
-    wanted is None; outputs are float32 [rows]."""
+    wanted is None; outputs are float32 [rows].  workspace: a uint8 tensor of dare_k_logprobs_workspace() bytes to use instead of one of the
+    call's own."""
     import torch
     if logits.dim() != 2 or (top_ids is None) != (top_logprobs is None) or (top_ids is not None and top_ids.dim() != 2):
         raise ValueError("logits must be a matrix, top_ids and top_logprobs both matrices or None")
@@ -805,7 +811,24 @@ def dare_k_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_ids=No
     call = _pack(_LOGPROBS_CALL, code, rows, vocab, top, scale, ld, px, 0 if tokens is None else _vector("tokens", tokens, i32, device, rows),
                  0 if logprobs is None else _vector("logprobs", logprobs, f32, device, rows),
                  0 if entropy is None else _vector("entropy", entropy, f32, device, rows), pi, pt)
-    _enqueue(device, stream, lib().dare_k_logprobs, call)
+    if workspace is None:
+        need = ctypes.c_size_t()
+        st = lib().dare_k_logprobs_workspace(call, need)
+        if st:
+            _check(st)
+        if need.value:
+            workspace = _scratch(need.value, logits.device, stream)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on cuda:%d" % device)
+    pw, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _enqueue(device, stream, lib().dare_k_logprobs, call, pw, size)
+
+
+def dare_k_logprobs_workspace(dtype, rows, vocab, top):
+    """Bytes of the workspace of a dare_k_logprobs call of these sizes (0: none)."""
+    need = ctypes.c_size_t()
+    _check(lib().dare_k_logprobs_workspace(_pack(_LOGPROBS_CALL, dtype, rows, vocab, top, 1.0, vocab, *[0] * 6), ctypes.byref(need)))
+    return need.value
 
 
 def _scratch(n_bytes, device, stream):

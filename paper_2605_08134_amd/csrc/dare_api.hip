@@ -1338,7 +1338,9 @@ dare_status dare_k_linear_q8(const dare_linear_q8_call* call, void* hip_stream) 
   return launched(launch_linear_q8(c.dtype, a, static_cast<hipStream_t>(hip_stream)), "dare_k_linear_q8");
 }
 
-dare_status dare_k_logprobs(const dare_logprobs_call* call, void* hip_stream) {
+namespace {
+// what a call and the query of its workspace both check
+dare_status check_logprobs(const dare_logprobs_call* call) {
   if (!call || call->struct_size != sizeof(dare_logprobs_call)) return refuse("null call, or struct_size does not match this library");
   const dare_logprobs_call& c = *call;
   if (c.dtype != DARE_F32 && c.dtype != DARE_BF16) return refuse("unknown dtype");
@@ -1349,6 +1351,21 @@ dare_status dare_k_logprobs(const dare_logprobs_call* call, void* hip_stream) {
   if (c.n_rows > 1 << 21 || c.vocab > 1 << 28) return unsupported("more than 2^21 rows or 2^28 logits in a row");
   if (c.ld < c.vocab) return refuse("ld below the width of a row");
   if (c.ld > 1l << 32) return unsupported("ld beyond 2^32");
+  return DARE_OK;
+}
+}  // namespace
+
+dare_status dare_k_logprobs_workspace(const dare_logprobs_call* call, size_t* bytes) {
+  if (!bytes) return refuse("null pointer");
+  const dare_status st = check_logprobs(call);
+  *bytes = st == DARE_OK ? logprobs_workspace(call->n_rows, call->vocab, call->top) : 0;
+  return st;
+}
+
+dare_status dare_k_logprobs(const dare_logprobs_call* call, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const dare_status st = check_logprobs(call);
+  if (st != DARE_OK) return st;
+  const dare_logprobs_call& c = *call;
   if (c.n_rows == 0) return DARE_OK;
   if (!c.logits || (c.top > 0 && (!c.top_ids || !c.top_logprobs))) return refuse("null pointer");
   if ((c.tokens == nullptr) != (c.logprobs == nullptr)) return refuse("tokens and their log-probabilities go together");
@@ -1367,7 +1384,11 @@ dare_status dare_k_logprobs(const dare_logprobs_call* call, void* hip_stream) {
   a.entropy = c.entropy;
   a.top_ids = c.top_ids;
   a.top_logprobs = c.top_logprobs;
+  a.workspace = workspace;
   if (!a.logprobs && !a.entropy && a.top == 0) return DARE_OK;
+  const size_t need = logprobs_workspace(c.n_rows, c.vocab, c.top);
+  if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0))
+    return refuse("workspace missing, too small or not on a 16-byte boundary");
   return launched(launch_logprobs(c.dtype, a, static_cast<hipStream_t>(hip_stream)), "dare_k_logprobs");
 }
 

@@ -211,8 +211,10 @@ struct LogprobsArgs {
   float* entropy;          // or nullptr
   int32_t* top_ids;        // [rows, top]
   float* top_logprobs;
+  void* workspace;         // logprobs_workspace() bytes of it
 };
 constexpr int kTopMost = 32;
+size_t logprobs_workspace(int rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s);
 
 struct RopeArgs {

@@ -8,6 +8,7 @@
 // In the pass a lane keeps only its largest chunk (16 bytes) and where that lies.  Take T, the k-th largest of the lanes' keys, or a lower one:
 // an element below T has k better ones, so the alternatives lie in the lanes whose key is T or more, about k of them; those lanes' elements are
 // read again (k / 1024 of the row), the ones from T on are listed, and a listed element's rank is how many others are above it.
+// Few rows: parts of a row by a workgroup each, and a second launch that joins what they found.
 // The list may overflow where many of the largest logits fall into the same few lanes; then the alternatives are found one after the other.
 #include <type_traits>
 
@@ -30,9 +31,16 @@ struct LogprobsDev {
   float* entropy;
   int32_t* top_ids;
   float* top_logprobs;
+  // rows cut into parts of part_len elements: of every part its sums, and the keys of its `top` largest elements, 0 where it has fewer
+  int parts, part_len;
+  f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part (WIDE)
+  unsigned long long* part_keys;
 };
 
-constexpr int kListed = 2048;   // elements that the list holds
+// What a workgroup does: a row, a part of one, or the joining of a row's parts (the row itself, where some part's sums say nothing)
+enum class Does { kRow, kPart, kJoin };
+
+constexpr int kMostParts = 16, kListed = 2048;   // elements that the list holds
 constexpr int kAhead = 4;       // chunks of a lane in flight
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
@@ -87,7 +95,7 @@ __device__ __forceinline__ Sums join(Sums a, float c) {
   return {a.r, over_lanes<0, TO>(a.s, add), over_lanes<0, TO>(a.t, add)};
 }
 
-template <typename T, int THREADS>
+template <typename T, int THREADS, Does DOES>
 __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) {
   constexpr int WAVES = THREADS / 64, E = 16 / sizeof(T);
   // a wave's largest keys: enough for the k-th largest, and so many that it is near it
@@ -97,17 +105,87 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
   __shared__ int lanes[THREADS], n_lanes, n_listed;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long row = blockIdx.x;
-  const T* x = p.x + row * p.ld;
+  const long row = DOES == Does::kPart ? blockIdx.x / p.parts : blockIdx.x;
+  const int offset = DOES == Does::kPart ? (int)(blockIdx.x % p.parts) * p.part_len : 0;
+  const int vocab = DOES == Does::kPart && p.vocab - offset > p.part_len ? p.part_len : p.vocab - offset;
+  const int top = p.top;
+  const T* x = p.x + row * p.ld + offset;
   const float c = p.scale * kLog2e;
   // elements in front of the first 16-byte boundary, whole chunks, elements behind the last one
   const int to_boundary = (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T);
-  const int head = to_boundary < p.vocab ? to_boundary : p.vocab;
-  const int chunks = (p.vocab - head) / E, singles = p.vocab - chunks * E;
+  const int head = to_boundary < vocab ? to_boundary : vocab;
+  const int chunks = (vocab - head) / E, singles = vocab - chunks * E;
   const T* body = x + head;
   auto single_place = [&](int i) { return i < head ? i : i + chunks * E; };
   auto chunk = [&](int i) { return reinterpret_cast<const u32x4*>(body)[i]; };
   if (tid == 0) n_lanes = n_listed = 0;
+
+  Sums all;
+  bool wide = false;
+  // (a NaN, or the difference of two infinities, is in the sum)
+  auto undefined = [&]() { return !(all.s >= 0.f); };
+  auto logprob = [&](float v) {
+    if (undefined()) return __builtin_nanf("");
+    if (v == -INFINITY) return -INFINITY;
+    const float log2_sum = __log2f(all.s);
+    if (wide) return (v - all.r) * p.scale - kLn2 * log2_sum;
+    const float d = fmaf(v, c, -all.r) - log2_sum;
+    return d > -INFINITY ? kLn2 * d : fmaf(v, p.scale, -kLn2 * all.r);  // (c v beyond fp32, scale v perhaps not)
+  };
+  float token_logit = -INFINITY;  // (read ahead of all else: two reads in a row)
+  if (DOES != Does::kPart && p.tokens && tid == 0) {
+    const int token = p.tokens[row];
+    if (token >= 0 && token < p.vocab) token_logit = (float)x[token];
+  }
+  auto put_sums = [&]() {
+    if (tid != 0) return;
+    if (p.tokens) p.logprobs[row] = logprob(token_logit);
+    if (p.entropy)
+      p.entropy[row] = undefined() ? __builtin_nanf("") : all.s == 0.f ? 0.f : fmaxf(kLn2 * (__log2f(all.s) - all.t / all.s), 0.f);
+  };
+  // the alternative of rank i, 0: there is none
+  auto put = [&](int i, u64 key) {
+    if constexpr (DOES == Does::kPart) {
+      p.part_keys[(long)blockIdx.x * top + i] = key;
+    } else {
+      p.top_ids[row * top + i] = key && !undefined() ? (int32_t)~(unsigned)key : -1;
+      p.top_logprobs[row * top + i] = logprob(key ? key_value(key) : -INFINITY);
+    }
+  };
+  auto put_listed = [&](int n) {
+    for (int i = tid; i < n; i += THREADS) {
+      const u64 own = listed[i];
+      int above = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) above += listed[j] > own;
+      if (above < top) put(above, own);
+    }
+  };
+  if constexpr (DOES == Does::kJoin) {
+    static_assert(kMostParts * kTopMost <= 2 * THREADS && kMostParts <= 64, "two keys per thread, a part per lane");
+    const int n = p.parts * top;  // at most 2 THREADS
+    const f32x4 part = lane < p.parts ? p.part_sums[row * p.parts + lane] : f32x4{-__FLT_MAX__, 0.f, 0.f, 0.f};
+    u64 keys[2], from = ~0ull;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) keys[k] = tid + k * THREADS < n ? p.part_keys[row * n + tid + k * THREADS] : 0;
+    // every part has this many keys from its own limit on, so the lowest limit has `top` keys from it on
+    if (top > 0 && lane < p.parts) from = p.part_keys[(row * p.parts + lane) * top + (top - 1) / p.parts];
+    if (!__any(part[3] != 0.f)) {
+      all = join<false>(Sums{part[0], part[1], part[2]}, c);
+      put_sums();
+      if (top == 0) return;
+      from = over_lanes(from, [](u64 a, u64 b) { return a < b ? a : b; });
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (keys[k] != 0 && keys[k] >= from) listed[atomicAdd(&n_listed, 1)] = keys[k];
+      __syncthreads();
+      const int found = n_listed;
+      put_listed(found);
+      if (tid >= found && tid < top) put(tid, 0);
+      return;
+    }
+  }
 
   float best = -INFINITY;  // largest element, and the first place of its chunk
   unsigned place = 0;
@@ -168,7 +246,6 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
     return join<decltype(wide)::value, WAVES == 16 ? 4 : 2>(wave_sums[lane % WAVES], c);
   };
   pass(std::false_type{});
-  const int top = p.top;
   u64 key = best > -INFINITY ? order_key(best, place) : 0;
   if (top > 0) {
     const int most = (top + WAVES - 1) / WAVES > 4 ? (top + WAVES - 1) / WAVES : top < 4 ? top : 4;
@@ -204,43 +281,22 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
     }
   }
   __syncthreads();
-  Sums all = joined(std::false_type{});
+  all = joined(std::false_type{});
   // no sum: no element, one that is not finite, or a c x beyond fp32
-  const bool wide = !(all.s > 0.f);
-  if (wide) {
-    __syncthreads();
-    pass(std::true_type{});
-    __syncthreads();
-    all = joined(std::true_type{});
-  }
-  // (a NaN, or the difference of two infinities, is in the sum)
-  const bool undefined = !(all.s >= 0.f), empty = all.s == 0.f;
-  const float log2_sum = __log2f(all.s);
-  auto logprob = [&](float v) {
-    if (undefined) return __builtin_nanf("");
-    if (v == -INFINITY) return -INFINITY;
-    if (wide) return (v - all.r) * p.scale - kLn2 * log2_sum;
-    const float d = fmaf(v, c, -all.r) - log2_sum;
-    return d > -INFINITY ? kLn2 * d : fmaf(v, p.scale, -kLn2 * all.r);  // (c v beyond fp32, scale v perhaps not)
-  };
-  if (tid == 0) {
-    if (p.tokens) {
-      const int token = p.tokens[row];
-      p.logprobs[row] = logprob(token >= 0 && token < p.vocab ? (float)x[token] : -INFINITY);
+  wide = !(all.s > 0.f);
+  if constexpr (DOES == Does::kPart) {
+    if (wide) wide = __syncthreads_or(best > -INFINITY) || undefined();  // (without an element the sums are right)
+    if (tid == 0) p.part_sums[blockIdx.x] = f32x4{all.r, all.s, all.t, wide ? 1.f : 0.f};
+  } else {
+    if (wide) {
+      __syncthreads();
+      pass(std::true_type{});
+      __syncthreads();
+      all = joined(std::true_type{});
     }
-    if (p.entropy) p.entropy[row] = undefined ? __builtin_nanf("") : empty ? 0.f : fmaxf(kLn2 * (log2_sum - all.t / all.s), 0.f);
+    put_sums();
   }
   if (top == 0) return;
-
-  int32_t* ids = p.top_ids + row * top;
-  float* tops = p.top_logprobs + row * top;
-  if (undefined) {
-    if (tid < top) {
-      ids[tid] = -1;
-      tops[tid] = __builtin_nanf("");
-    }
-    return;
-  }
   const u64 from = limit;
   if (key >= from) lanes[atomicAdd(&n_lanes, 1)] = tid;
   __syncthreads();
@@ -265,26 +321,14 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
   elements([&](float v, int first, int e) {
     if (v > -INFINITY && order_key(v, first) >= from) {
       const int at = atomicAdd(&n_listed, 1);
-      if (at < kListed) listed[at] = order_key(v, first + e);
+      if (at < kListed) listed[at] = order_key(v, offset + first + e);
     }
   });
   __syncthreads();
   const int found = n_listed;
   if (found <= kListed) {
-    for (int i = tid; i < found; i += THREADS) {
-      const u64 own = listed[i];
-      int above = 0;
-#pragma unroll 8
-      for (int j = 0; j < found; ++j) above += listed[j] > own;
-      if (above < top) {
-        ids[above] = (int32_t)~(unsigned)own;
-        tops[above] = logprob(key_value(own));
-      }
-    }
-    if (tid >= found && tid < top) {
-      ids[tid] = -1;
-      tops[tid] = -INFINITY;
-    }
+    put_listed(found);
+    if (tid >= found && tid < top) put(tid, 0);
     return;
   }
   // more than the list holds: one after the other (there are more than `top`)
@@ -292,7 +336,7 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
   for (int k = 0; k < top; ++k) {
     u64 next = 0;
     elements([&](float v, int first, int e) {
-      const u64 own = v > -INFINITY ? order_key(v, first + e) : 0;
+      const u64 own = v > -INFINITY ? order_key(v, offset + first + e) : 0;
       if (own < last && own > next) next = own;
     });
     next = wave_max(next);
@@ -301,11 +345,18 @@ __global__ void __launch_bounds__(THREADS, 8) logprobs_kernel(LogprobsDev<T> p) 
     __syncthreads();
     next = wave_max(wave_keys[lane % WAVES]);
     last = next;
-    if (tid == 0) {
-      ids[k] = (int32_t)~(unsigned)last;
-      tops[k] = logprob(key_value(last));
-    }
+    if (tid == 0) put(k, last);
   }
+}
+
+// Few rows are cut so that their parts give every CU a workgroup, into pieces that a workgroup loads at once.  One workgroup takes 126464 logits at 16
+// a ns, a part of 8192 costs it 2 us, and the second launch 3 to 5 (us, bf16, uncut and cut: 1 x 126464 with 2 alternatives 12.5 8.2, with 32
+// 14.4 12.9, 32 x 126464 with 8 14.8 11.3, 64 x 126464 in four parts 14.9 13.7, in three 85 x 126464 16.0 16.7; 1 x 32768 6.5 7.4).
+int logprobs_parts(int rows, int vocab) {
+  if (vocab < 65536) return 1;
+  int n = 256 / rows < vocab / 8192 ? 256 / rows : vocab / 8192;
+  if (n > kMostParts) n = kMostParts;
+  return n < 4 ? 1 : n;
 }
 
 template <typename T>
@@ -321,14 +372,33 @@ hipError_t launch(const LogprobsArgs& a, hipStream_t s) {
   p.entropy = a.entropy;
   p.top_ids = a.top_ids;
   p.top_logprobs = a.top_logprobs;
-  if (a.vocab < 16384)
-    hipLaunchKernelGGL((logprobs_kernel<T, 256>), dim3(a.rows), dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((logprobs_kernel<T, 1024>), dim3(a.rows), dim3(1024), 0, s, p);
+  p.parts = logprobs_parts(a.rows, a.vocab);
+  if (p.parts > 1) {
+    // (parts begin on 16-byte boundaries if the row does)
+    p.part_len = ((a.vocab + p.parts - 1) / p.parts + 63) / 64 * 64;
+    p.part_sums = reinterpret_cast<f32x4*>(a.workspace);
+    p.part_keys = reinterpret_cast<unsigned long long*>(p.part_sums + (long)a.rows * p.parts);
+    if (p.part_len < 16384)
+      hipLaunchKernelGGL((logprobs_kernel<T, 256, Does::kPart>), dim3(a.rows * p.parts), dim3(256), 0, s, p);
+    else
+      hipLaunchKernelGGL((logprobs_kernel<T, 1024, Does::kPart>), dim3(a.rows * p.parts), dim3(1024), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((logprobs_kernel<T, 256, Does::kJoin>), dim3(a.rows), dim3(256), 0, s, p);
+  } else if (a.vocab < 16384) {
+    hipLaunchKernelGGL((logprobs_kernel<T, 256, Does::kRow>), dim3(a.rows), dim3(256), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((logprobs_kernel<T, 1024, Does::kRow>), dim3(a.rows), dim3(1024), 0, s, p);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
+
+size_t logprobs_workspace(int rows, int vocab, int top) {
+  const int parts = rows > 0 ? logprobs_parts(rows, vocab) : 1;
+  return parts > 1 ? (size_t)rows * parts * (sizeof(f32x4) + top * sizeof(u64)) : 0;
+}
 
 hipError_t launch_logprobs(int dtype, const LogprobsArgs& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;

@@ -341,6 +341,56 @@ def test_logprobs_parts_that_are_left_out_and_no_rows():
     B.dare_k_logprobs(x[:0], tokens[:0], part[0][:0], part[1][:0], part[2][:0], part[3][:0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab,pad", [(1, 126464, 0), (1, 126465, 3), (2, 33001, 1), (7, 65536, 0), (16, 131072, 0), (17, 90001, 1), (64, 70000, 8), (65, 70000, 0)])
+@pytest.mark.parametrize("top", [0, 1, 8, 32])
+def test_logprobs_of_few_rows_with_a_workspace(dtype, rows, vocab, pad, top):
+    """A row's result does not depend on what is in the workspace, nor, but for roundings, on the parts it is cut into."""
+    g = _gen(rows + vocab)
+    x = (torch.randn(rows, vocab, generator=g) * 3).to(TYPES[dtype])
+    x[0, :vocab // 2] = -math.inf
+    x[0, vocab - 9000:] = -math.inf
+    x[rows - 1, 100:5000] = 12.0
+    tokens = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    got = _outputs(rows, top)
+    code = B.DARE_BF16 if dtype == "bf16" else B.DARE_F32
+    need = B.dare_k_logprobs_workspace(code, rows, vocab, top)
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    B.dare_k_logprobs(_padded(x, pad, float("nan")), tokens.cuda(), *got, workspace=ws)
+    _check(x, tokens, 1.0, top, got)
+    assert (ws[need:] == 255).all()
+    if top == 32:     # the same rows among many
+        many = _outputs(300, top)
+        big = torch.cat([x.cuda(), x[:1].cuda().expand(300 - rows, vocab)]) if 300 * vocab * x.element_size() < 1 << 28 else None
+        if big is not None:
+            B.dare_k_logprobs(big, tokens.repeat(300 // rows + 1)[:300].cuda(), *many)
+            assert torch.equal(many[2][:rows], got[2]) and torch.allclose(many[3][:rows], got[3], rtol=0, atol=1e-4)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logprobs_special_parts(dtype):
+    """Parts without an element, with NaN or infinity, and with values at the ends of the type, beside ordinary ones."""
+    vocab, top = 126464, 5
+    lowest = float(torch.finfo(TYPES[dtype]).min)
+    x = torch.randn(8, vocab, generator=_gen(8)).to(TYPES[dtype])
+    x[0] = -math.inf
+    x[1], x[1, 70000] = -math.inf, 2.0
+    x[2, 126463] = math.nan
+    x[3, 0] = math.inf
+    x[4, :100000] = lowest
+    x[5] = lowest
+    x[6, 60000:] = -math.inf
+    x[6, :8192] = -math.inf
+    x[7, 9] = -lowest
+    tokens = torch.tensor([5, 70000, 1, 1, 3, 4, 9000, 9], dtype=torch.int32)
+    got = _outputs(8, top)
+    B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got)
+    for r in (2, 3):
+        assert torch.isnan(got[0][r]) and torch.isnan(got[1][r]) and (got[2][r] == -1).all() and torch.isnan(got[3][r]).all()
+    keep = [0, 1, 4, 5, 6, 7]
+    _check(x[keep], tokens[keep], 1.0, top, [t[torch.tensor(keep).cuda()] for t in got])
+
+
 def test_logprobs_many_rows_of_few_logits():
     x = torch.randn(70001, 33, generator=_gen(4)).bfloat16()
     tokens = torch.randint(0, 33, (70001,), generator=_gen(5), dtype=torch.int32)

@@ -72,18 +72,36 @@ LOGPROBS = dict(size=B._LOGPROBS_CALL.size, dtype=B.DARE_F32, rows=3, vocab=100,
     (dict(rows=(1 << 21) + 1), UNSUPPORTED), (dict(vocab=(1 << 28) + 1, ld=1 << 29), UNSUPPORTED), (dict(ld=(1 << 32) + 1), UNSUPPORTED),
 ])
 def test_logprobs_refuses(L, change, want):
-    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*dict(LOGPROBS, **change).values()), None) == want
+    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*dict(LOGPROBS, **change).values()), None, 0, None) == want
     assert L.dare_last_error(None)
 
 
+def test_logprobs_workspace(L):
+    """Few rows of many logits are cut into parts and need a workspace; a call without it, or with one too small or not aligned, is refused."""
+    need = B.dare_k_logprobs_workspace(B.DARE_BF16, 1, 126464, 2)
+    assert need > 0 and need % 16 == 0
+    assert B.dare_k_logprobs_workspace(B.DARE_BF16, 1, 126464, 0) < need < B.dare_k_logprobs_workspace(B.DARE_BF16, 3, 126464, 2)
+    for rows, vocab in ((0, 126464), (1, 1000), (300, 126464), (1 << 21, 1 << 28)):
+        assert B.dare_k_logprobs_workspace(B.DARE_F32, rows, vocab, 32) == 0
+    for rows in range(1, 257):
+        for vocab in (16384, 40000, 126464, 1 << 28):
+            assert B.dare_k_logprobs_workspace(B.DARE_F32, rows, vocab, 32) <= 256 * (16 + 8 * 32)
+    few = dict(LOGPROBS, dtype=B.DARE_BF16, rows=1, vocab=126464, ld=126464)
+    call = B._LOGPROBS_CALL.pack(*few.values())
+    for ws, size in ((None, 0), (P, need - 1), (P + 8, need)):
+        assert L.dare_k_logprobs(call, ws, size, None) == INVALID
+    assert L.dare_k_logprobs_workspace(call, None) == INVALID
+    with pytest.raises(B.DareError):
+        B.dare_k_logprobs_workspace(B.DARE_BF16, 1, 126464, 33)
+
+
 def test_no_call_and_no_rows(L):
-    for name in ("dare_k_norm_q8", "dare_k_linear_q8", "dare_k_logprobs"):
-        assert getattr(L, name)(None, None) == INVALID
+    assert L.dare_k_norm_q8(None, None) == L.dare_k_linear_q8(None, None) == L.dare_k_logprobs(None, None, 0, None) == INVALID
     assert L.dare_k_norm_q8(B._NORM_Q8_CALL.pack(*dict(NORM, rows=0, x=0, codes=0, scales=0, gain=0).values()), None) == B.DARE_OK
     assert L.dare_k_linear_q8(B._LINEAR_Q8_CALL.pack(*dict(LINEAR, m=0, a=0, wt=0, out=0).values()), None) == B.DARE_OK
-    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*dict(LOGPROBS, rows=0, logits=0).values()), None) == B.DARE_OK
+    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*dict(LOGPROBS, rows=0, logits=0).values()), None, 0, None) == B.DARE_OK
     nothing = dict(LOGPROBS, top=0, tokens=0, logprobs=0, entropy=0, top_ids=0, top_logprobs=0)
-    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*nothing.values()), None) == B.DARE_OK
+    assert L.dare_k_logprobs(B._LOGPROBS_CALL.pack(*nothing.values()), None, 0, None) == B.DARE_OK
 
 
 def test_structs_of_the_binding_are_those_of_the_header(tmp_path):
