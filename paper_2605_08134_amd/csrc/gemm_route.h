@@ -178,14 +178,40 @@ constexpr GemmRoute linear_route(int m, int n, int k) {
   return gemm_route(m, n, k, 1, false);
 }
 
-// 8-bit codes: the shapes of linear_route for the same bytes of k (k in units of two codes).  The wide tiles are the four-wave ones, where they can
-// run (bf16 outputs, three k-steps); 128 x 192 stands for the others.
+// 8-bit codes (k in units of two): what a shape costs in bytes and cycles per k-step is what it costs in bf16, so the costs are those of best_tile, the
+// wide tiles in their four-wave form (quad_cost), which is there for bf16 outputs and three k-steps.  A sum has half as many k-steps, starts and ends
+// weigh twice as much, and few rows want more and smaller workgroups than in bf16:
+//   * up to 8 rows of up to 4096 columns, one workgroup per 16 columns on the 256 CUs: the stream over the weights (us, it and 32 x 32: 1 x 4096 x 4096 6.7
+//     7.3, 8 x 1024 x 512 2.7 2.9; on the other side 5 x 4416 x 4352 11.0 7.7, 16 x 4096 x 4096 8.2 8.1);
+//   * as long as one round is enough for them, 32 x 32, then 64 x 32, then 64 x 64 (64 x 4096 x 12288 19.7, 26.9 and more, 105 x 3648 x 6272 14.7 14.4 17.2, 143 x 3648
+//     x 2048 8.9 8.7 7.3).
+// Over 287 sizes (1 to 16384 rows, 384 to 126464 columns, k 384 to 12288) the shape taken is on average 0.7 % behind the fastest, at most 12 % (10 x 896 x
+// 640 3.05 and 2.71).
 constexpr GemmRoute linear_q8_route(int m, int n, int k, bool bf16) {
-  const GemmRoute r = linear_route(m, n, k);
   const bool quad = bf16 && k / kRouteBK >= kQuadMinSteps;
-  if (r == GemmRoute::kPp192 || r == GemmRoute::kQuad192) return quad ? GemmRoute::kQuad192 : GemmRoute::k128x192;
-  if (r == GemmRoute::kPp256 || r == GemmRoute::kQuad256) return quad ? GemmRoute::kQuad256 : GemmRoute::k128x192;
-  return r == GemmRoute::kPp128 ? GemmRoute::k128x128 : r;
+  if (m <= 8 && n <= 4096) return GemmRoute::kSkinny;
+  if (tiles_of(m, n, 32, 32) <= 256) return GemmRoute::k32x32;
+  if (tiles_of(m, n, 64, 32) <= 256) return GemmRoute::k64x32;
+  if (tiles_of(m, n, 64, 64) <= 256) return GemmRoute::k64x64;
+  if (tiles_of(m, n, kPpRows, 256) > 8192) return quad ? GemmRoute::kQuad256 : GemmRoute::k128x192;  // (the costs below stay in 32 bits)
+  GemmRoute best = GemmRoute::k64x64;
+  int least = tile_cost(m, n, 64, 64, 153, 229);
+  auto offer = [&](GemmRoute r, int cost) {
+    if (cost < least) {
+      least = cost;
+      best = r;
+    }
+  };
+  offer(GemmRoute::k64x96, tile_cost(m, n, 64, 96, 235, 306));
+  offer(GemmRoute::k64x128, tile_cost(m, n, 64, 128, 280, 364));
+  offer(GemmRoute::k128x96, tile_cost(m, n, 128, 96, 390, 448));
+  offer(GemmRoute::k128x128, tile_cost(m, n, 128, 128, 490, 564));
+  offer(GemmRoute::k128x192, tile_cost(m, n, 128, 192, 780, 897));
+  if (quad) {
+    offer(GemmRoute::kQuad192, tile_cost(m, n, kPpRows, 192, 1050, 1050));
+    offer(GemmRoute::kQuad256, tile_cost(m, n, kPpRows, 256, 1290, 1290));
+  }
+  return best;
 }
 
 // What a launch of `tiles` tiles takes where it is compared with one of another number of tiles: rounds of the CUs above all, idle CUs
