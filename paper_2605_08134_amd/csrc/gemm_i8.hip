@@ -109,7 +109,8 @@ hipError_t launch(const LinearQ8Dev& p, hipStream_t s) {
       return hipGetLastError();
     case GemmRoute::k32x32: return launch_tile16<T, 32, 32, 2, 2, 8>(p, s);
     case GemmRoute::k64x32: return launch_tile16<T, 64, 32, 4, 2, 6>(p, s);
-    case GemmRoute::k64x64: return launch_tile16<T, 64, 64, 2, 4, 8>(p, s);
+    case GemmRoute::k32x64: return launch_tile16<T, 32, 64, 1, 4, 6>(p, s);
+    case GemmRoute::k64x64: return launch_tile16<T, 64, 64, 2, 4, 4>(p, s);
     case GemmRoute::k64x96: return launch_tile16<T, 64, 96, 4, 2, 6>(p, s);
     case GemmRoute::k64x128: return launch_tile16<T, 64, 128, 2, 4, 5>(p, s);
     case GemmRoute::k128x96: return launch_tile16<T, 128, 96, 4, 2, 4>(p, s);

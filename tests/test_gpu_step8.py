@@ -175,13 +175,12 @@ def test_linear_q8(act, dtype, m, n, k, extras):
     assert ou.worst(_linear(a, sa, wt, sw, bias, act, res, dtype), want, bound) <= 1.0
 
 
-# every shape of the launch: rows, columns and k (in units of two codes) of the bf16 projection's list
-@pytest.mark.parametrize("route,m,n,half_k", ou.LINEAR_SHAPES)
+@pytest.mark.parametrize("shape,m,n,k", su.LINEAR_Q8_SHAPES)
 @pytest.mark.parametrize("dtype,act,extras", [("bf16", None, False), ("bf16", "gelu", True), ("f32", "silu", True)])
-def test_linear_q8_in_every_shape(route, m, n, half_k, dtype, act, extras):
+def test_linear_q8_in_every_shape(shape, m, n, k, dtype, act, extras):
     g = torch.Generator(device="cuda").manual_seed(m + n)
     codes = lambda *s: torch.randint(-127, 128, s, generator=g, dtype=torch.int8, device="cuda")
-    td, k = TYPES[dtype], 2 * half_k
+    td = TYPES[dtype]
     a, wt, sa, sw = codes(m, k), codes(n, k), torch.rand(m, generator=g, device="cuda") * 0.02, torch.rand(n, generator=g, device="cuda") * 0.02
     rn = lambda *s: torch.randn(s, generator=g, device="cuda").to(td)
     bias, res = (rn(n), rn(m, n)) if extras else (None, None)

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 from paper_2605_08134_amd import binding as B
+import step8_util as su
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 P = 0x1000      # never dereferenced: the checks come first
@@ -155,7 +156,7 @@ int main() {
           const bool wide = r == GemmRoute::kQuad192 || r == GemmRoute::kQuad256;
           if (wide && (!bf16 || k < 192)) ++bad;
           switch (r) {
-            case GemmRoute::kSkinny: case GemmRoute::k32x32: case GemmRoute::k64x32: case GemmRoute::k64x64: case GemmRoute::k64x96:
+            case GemmRoute::kSkinny: case GemmRoute::k32x32: case GemmRoute::k64x32: case GemmRoute::k32x64: case GemmRoute::k64x64: case GemmRoute::k64x96:
             case GemmRoute::k64x128: case GemmRoute::k128x96: case GemmRoute::k128x128: case GemmRoute::k128x192: case GemmRoute::kQuad192:
             case GemmRoute::kQuad256: seen |= 1 << (int)r; break;
             default: ++bad;
@@ -166,4 +167,16 @@ int main() {
     csrc = os.path.join(ROOT, "paper_2605_08134_amd", "csrc")
     subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "route.cpp"), "-o", str(tmp_path / "route")], check=True)
     bad, shapes = subprocess.run([str(tmp_path / "route")], capture_output=True, text=True, check=True).stdout.split()
-    assert int(bad) == 0 and int(shapes) == 11
+    assert int(bad) == 0 and int(shapes) == 12
+
+
+def test_shapes_that_the_gpu_tests_name(tmp_path):
+    src = '#include <cstdio>\n#include "gemm_route.h"\nusing namespace dare;\nint main() {\n'
+    for shape, m, n, k in su.LINEAR_Q8_SHAPES:
+        src += "  std::printf(\"%%d \", linear_q8_route(%d, %d, %d, true) == GemmRoute::%s);\n" % (m, n, k // 2, shape)
+    (tmp_path / "names.cpp").write_text(src + "}\n")
+    csrc = os.path.join(ROOT, "paper_2605_08134_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "names.cpp"), "-o", str(tmp_path / "names")], check=True)
+    got = subprocess.run([str(tmp_path / "names")], capture_output=True, text=True, check=True).stdout.split()
+    assert got == ["1"] * len(su.LINEAR_Q8_SHAPES)
+    assert len({s[0] for s in su.LINEAR_Q8_SHAPES}) == 12
