@@ -6,9 +6,10 @@
 // 3e-5, and a row's codes would hang on the order in which its sum of squares was formed: one code in 10^5 goes to a neighbour, and
 // no other program could say which.
 //
-// Memory-bound: one read of x and o, one write of s and of a byte per channel.  A row is held in registers, as 64-bit values, from its
-// load to its codes, by a wave (rows of up to 2048 channels) or a workgroup of four waves (up to 16384); longer rows are read once per
-// pass.
+// Memory-bound: one read of x and o, one write of s and of a byte per channel.  A row is held in registers from its load to its codes, by
+// 8 to 64 lanes (rows of up to 1024 channels) or a workgroup of four waves (up to 16384); longer rows are read once per pass.
+#include <type_traits>
+
 #include "dare_common.h"
 #include "lanes.h"
 
@@ -59,16 +60,16 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 
 __device__ __forceinline__ double add2(double a, double b) { return a + b; }
 __device__ __forceinline__ double max2(double a, double b) { return fmax(a, b); }
-// Over the lanes of a row: a wave's, or, with four waves, the workgroup's through LDS (`sh`: 4 values that nothing else uses)
-template <int WAVES, class F>
+// Over the lanes of a row: 8 to 64 neighbouring ones, or the workgroup's 256 through LDS (`sh`: 4 values that nothing else uses)
+template <int LANES, class F>
 __device__ __forceinline__ double reduce(double v, F f, double* sh) {
-  v = over_lanes(v, f);
-  if constexpr (WAVES > 1) {
+  constexpr int STEPS = LANES == 8 ? 3 : LANES == 16 ? 4 : LANES == 32 ? 5 : 6;
+  v = over_lanes<0, STEPS>(v, f);
+  if constexpr (LANES > 64) {
+    static_assert(LANES == 256, "four waves");
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = sh[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) v = f(v, sh[w]);
+    v = f(f(sh[0], sh[1]), f(sh[2], sh[3]));
   }
   return v;
 }
@@ -104,100 +105,124 @@ __device__ __forceinline__ RowScale row_scale(double largest, double rest, float
   return r;
 }
 
-// Rows of up to WAVES * 512 HOLD channels, 4 / WAVES of them per workgroup
-template <typename T, int KIND, int WAVES, int HOLD>
+// Rows of up to 8 LANES HOLD channels, LANES to a row.  y is held from the statistic to the codes where that takes few registers; of longer rows s is held,
+// which fp32 does, and y formed twice: fewer registers are more rows on a CU (2000 x 12288 bf16, rms with a sum 47.3 -> 45.0 us).
+template <typename T, int KIND, int LANES, int HOLD>
 __global__ void __launch_bounds__(256) norm_q8_kernel(NormQ8Dev<T> p) {
-  constexpr int LANES = WAVES * 64, ROWS = 4 / WAVES;
+  constexpr int ROWS = 256 / LANES;
+  constexpr bool NORM = KIND != DARE_NORM_NONE, LAYER = KIND == DARE_NORM_LAYER, TWICE = NORM && HOLD > 2;
   __shared__ double sh[4][4];
   const int lane = threadIdx.x % LANES;
   const long row = (long)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (row >= p.rows) return;  // (whole waves; with four waves per row no workgroup)
+  if (row >= p.rows) return;  // (all lanes of a row; no workgroup that shares one)
   const T* x = p.x + row * p.ldx;
   const T* o = p.o + row * p.ldo;
   const int groups = p.d >> 3;
-  double y[HOLD][8];
+  float s[HOLD][8];
+  Raw8 gain[HOLD], bias[HOLD];
   {
     Raw8 a[HOLD], b[HOLD];
 #pragma unroll
     for (int h = 0; h < HOLD; ++h) {
       const int g = lane + h * LANES;
-      a[h] = b[h] = Raw8{};
+      a[h] = b[h] = gain[h] = bias[h] = Raw8{};
       if (g < groups) {
         load8(x + g * 8, a[h]);
         if (p.o) load8(o + g * 8, b[h]);
       }
     }
+    if constexpr (NORM) {
+#pragma unroll
+      for (int h = 0; h < HOLD; ++h) {
+        const int g = lane + h * LANES;
+        if (g < groups) {
+          load8(p.gain + g * 8, gain[h]);
+          if (LAYER && p.bias) load8(p.bias + g * 8, bias[h]);
+        }
+      }
+    }
 #pragma unroll
     for (int h = 0; h < HOLD; ++h) {
       const int g = lane + h * LANES;
-      float v[8], w[8];
-      values8(x, a[h], v);
+      float w[8];
+      values8(x, a[h], s[h]);
       if (p.o) {
         values8(o, b[h], w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)(T)(v[e] + w[e]);
+        for (int e = 0; e < 8; ++e) s[h][e] = (float)(T)(s[h][e] + w[e]);
       }
-      if (p.x_out && g < groups) store8(p.x_out + row * p.ldxo + g * 8, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[h][e] = v[e];
+      if (p.x_out && g < groups) store8(p.x_out + row * p.ldxo + g * 8, s[h]);
     }
   }
-  if constexpr (KIND != DARE_NORM_NONE) {
-    double mean = 0.0, sum = 0.0;
-    if constexpr (KIND == DARE_NORM_LAYER) {
+  double mean = 0.0, r = 1.0;
+  if constexpr (NORM) {
+    double sum = 0.0;
+    if constexpr (LAYER) {
 #pragma unroll
       for (int h = 0; h < HOLD; ++h)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += y[h][e];
-      mean = reduce<WAVES>(sum, add2, sh[0]) / p.d;
+        for (int e = 0; e < 8; ++e) sum += s[h][e];
+      mean = reduce<LANES>(sum, add2, sh[0]) / p.d;
       sum = 0.0;
     }
 #pragma unroll
     for (int h = 0; h < HOLD; ++h)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (KIND == DARE_NORM_LAYER) y[h][e] = lane + h * LANES < groups ? y[h][e] - mean : 0.0;
-        sum = fma(y[h][e], y[h][e], sum);
+        const double v = LAYER ? lane + h * LANES < groups ? s[h][e] - mean : 0.0 : s[h][e];
+        sum = fma(v, v, sum);
       }
-    const double r = 1.0 / sqrt(reduce<WAVES>(sum, add2, sh[1]) / p.d + p.eps);
+    r = 1.0 / sqrt(reduce<LANES>(sum, add2, sh[1]) / p.d + p.eps);
+  }
+  // y of 8 channels (behind the row's end 0: their gain and bias are)
+  auto normed = [&](int h, double (&y)[8]) __attribute__((always_inline)) {
+    float g[8], b[8];
+    values8(x, gain[h], g);
+    values8(x, bias[h], b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = LAYER ? fma(s[h][e] - mean, r * g[e], (double)b[e]) : s[h][e] * (r * g[e]);
+  };
+  // rest: a NaN that stays if some value is not finite
+  double largest = 0.0, rest = 0.0, held[NORM && !TWICE ? HOLD : 1][8];
+  if constexpr (NORM) {
 #pragma unroll
     for (int h = 0; h < HOLD; ++h) {
-      const int g = lane + h * LANES;
-      if (g < groups) {
-        Raw8 t;
-        float v[8];
-        load8(p.gain + g * 8, t);
-        values8(x, t, v);
+      double y[8];
+      normed(h, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[h][e] *= r * v[e];
-        if constexpr (KIND == DARE_NORM_LAYER) {
-          if (p.bias) {
-            load8(p.bias + g * 8, t);
-            values8(x, t, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[h][e] += v[e];
-          }
-        }
+      for (int e = 0; e < 8; ++e) {
+        largest = fmax(largest, fabs(y[e]));
+        rest = fma(y[e], 0.0, rest);
+        if constexpr (!TWICE) held[h][e] = y[e];
       }
     }
+  } else {
+    float largest32 = 0.f, rest32 = 0.f;
+#pragma unroll
+    for (int h = 0; h < HOLD; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        largest32 = fmaxf(largest32, fabsf(s[h][e]));
+        rest32 = fmaf(s[h][e], 0.f, rest32);
+      }
+    largest = largest32;
+    rest = rest32;
   }
-  double largest = 0.0, rest = 0.0;  // rest: a NaN that stays if some value is not finite
-#pragma unroll
-  for (int h = 0; h < HOLD; ++h)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      largest = fmax(largest, fabs(y[h][e]));
-      rest = fma(y[h][e], 0.0, rest);
-    }
-  largest = reduce<WAVES>(largest, max2, sh[2]);
-  rest = reduce<WAVES>(rest, add2, sh[3]);
-  const RowScale s = row_scale(largest, rest, p.scales + row, lane == 0);
+  largest = reduce<LANES>(largest, max2, sh[2]);
+  rest = reduce<LANES>(rest, add2, sh[3]);
+  const RowScale q = row_scale(largest, rest, p.scales + row, lane == 0);
 #pragma unroll
   for (int h = 0; h < HOLD; ++h) {
     const int g = lane + h * LANES;
     int c[8];
+    double y[8];
+    if constexpr (TWICE) normed(h, y);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = s.finite ? code_of(y[h][e], s.scale, s.inverse) : 0;
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (!NORM) y[e] = s[h][e];
+      if constexpr (NORM && !TWICE) y[e] = held[h][e];
+      c[e] = q.finite ? code_of(y[e], q.scale, q.inverse) : 0;
+    }
     if (g < groups) *reinterpret_cast<u32x2*>(p.codes + row * p.ldc + g * 8) = pack8(c);
   }
 }
@@ -241,7 +266,7 @@ __global__ void __launch_bounds__(256) norm_q8_long_kernel(NormQ8Dev<T> p) {
       for (int e = 0; e < 8; ++e) sum += y[e];
     }
     summed = x_out != nullptr;
-    mean = reduce<4>(sum, add2, sh[0]) / p.d;
+    mean = reduce<256>(sum, add2, sh[0]) / p.d;
   }
   if constexpr (KIND != DARE_NORM_NONE) {
     double sum = 0.0;
@@ -251,7 +276,7 @@ __global__ void __launch_bounds__(256) norm_q8_long_kernel(NormQ8Dev<T> p) {
       for (int e = 0; e < 8; ++e) sum = fma(y[e] - mean, y[e] - mean, sum);
     }
     summed = x_out != nullptr;
-    r = 1.0 / sqrt(reduce<4>(sum, add2, sh[1]) / p.d + p.eps);
+    r = 1.0 / sqrt(reduce<256>(sum, add2, sh[1]) / p.d + p.eps);
   }
   auto value = [&](int g, double (&y)[8]) {
     sum_of(g, y);
@@ -280,8 +305,8 @@ __global__ void __launch_bounds__(256) norm_q8_long_kernel(NormQ8Dev<T> p) {
     }
   }
   summed = x_out != nullptr;
-  largest = reduce<4>(largest, max2, sh[2]);
-  rest = reduce<4>(rest, add2, sh[3]);
+  largest = reduce<256>(largest, max2, sh[2]);
+  rest = reduce<256>(rest, add2, sh[3]);
   const RowScale s = row_scale(largest, rest, p.scales + row, threadIdx.x == 0);
   for (int g = threadIdx.x; g < groups; g += 256) {
     value(g, y);
@@ -292,21 +317,26 @@ __global__ void __launch_bounds__(256) norm_q8_long_kernel(NormQ8Dev<T> p) {
   }
 }
 
+template <typename T, int KIND, int LANES, int HOLD>
+hipError_t launch_held(const NormQ8Dev<T>& p, hipStream_t s) {
+  constexpr int ROWS = 256 / LANES;
+  hipLaunchKernelGGL((norm_q8_kernel<T, KIND, LANES, HOLD>), dim3((p.rows + ROWS - 1) / ROWS), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
 template <typename T, int KIND>
 hipError_t launch(const NormQ8Dev<T>& p, hipStream_t s) {
-  const int rows4 = (p.rows + 3) / 4;
-  if (p.d <= 512)
-    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 1, 1>), dim3(rows4), dim3(256), 0, s, p);
-  else if (p.d <= 2048)
-    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 1>), dim3(p.rows), dim3(256), 0, s, p);
-  else if (p.d <= 4096)
-    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 2>), dim3(p.rows), dim3(256), 0, s, p);
-  else if (p.d <= 8192)
-    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 4>), dim3(p.rows), dim3(256), 0, s, p);
-  else if (p.d <= 16384)
-    hipLaunchKernelGGL((norm_q8_kernel<T, KIND, 4, 8>), dim3(p.rows), dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((norm_q8_long_kernel<T, KIND>), dim3(p.rows), dim3(256), 0, s, p);
+  if (p.d <= 64) return launch_held<T, KIND, 8, 1>(p, s);
+  if (p.d <= 128) return launch_held<T, KIND, 16, 1>(p, s);
+  if (p.d <= 256) return launch_held<T, KIND, 32, 1>(p, s);
+  if (p.d <= 512) return launch_held<T, KIND, 64, 1>(p, s);
+  if (p.d <= 1024) return launch_held<T, KIND, 64, 2>(p, s);
+  if (p.d <= 2048) return launch_held<T, KIND, 256, 1>(p, s);
+  if (p.d <= 4096) return launch_held<T, KIND, 256, 2>(p, s);
+  if (p.d <= 6144) return launch_held<T, KIND, 256, 3>(p, s);
+  if (p.d <= 8192) return launch_held<T, KIND, 256, 4>(p, s);
+  if (p.d <= 12288) return launch_held<T, KIND, 256, 6>(p, s);
+  if (p.d <= 16384) return launch_held<T, KIND, 256, 8>(p, s);
+  hipLaunchKernelGGL((norm_q8_long_kernel<T, KIND>), dim3(p.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
