@@ -270,7 +270,8 @@ dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspac
  *     y = s | (s - mean) / sqrt(var + eps) * gain + bias | s / sqrt(mean(s^2) + eps) * gain     (DARE_NORM_NONE | LAYER | RMS)
  *     scales[t] = max |y| / 127 rounded to fp32,  codes[t] = y / scales[t] to the nearest whole number, ties to even, in [-127, 127]
  * so that codes[t] * scales[t] stands for y.  Sums, y and the decision between two codes are formed in 64 bits.  A row of zeros has the scale 0
- * and codes 0; one with a value that is not finite the scale NaN and codes 0, and its projections are NaN.
+ * and codes 0; one with a value that is not finite (zeros under DARE_NORM_RMS with eps 0 are), or with a scale beyond fp32, the scale NaN and codes 0, and its
+ * projections are NaN.
  * The codes of a weight: DARE_NORM_NONE of the rows of the packed matrix (dare_k_pack_weight), one scale per output column.
  *   x, o, x_out  [n_rows, ldx | ldo | ldxo] dtype on 16-byte boundaries; o and x_out may be NULL; x_out may be x or o (with the same ld)
  *   gain, bias   [d] dtype on 16-byte boundaries; gain for both norms, bias (or NULL) for LAYER

@@ -94,11 +94,12 @@ struct RowScale {
   double scale, inverse;
   bool finite;
 };
-// largest: max |y|; rest: 0, or NaN where some y is not finite
+// largest: max |y|; rest: 0, or NaN where some y is not finite.  (A scale beyond fp32 is none either.)
 __device__ __forceinline__ RowScale row_scale(double largest, double rest, float* to, bool writes) {
   RowScale r;
-  r.finite = rest == 0.0;
-  const float scale = r.finite ? (float)(largest / 127.0) : __builtin_nanf("");
+  float scale = (float)(largest / 127.0);
+  r.finite = rest == 0.0 && scale < INFINITY;
+  if (!r.finite) scale = __builtin_nanf("");
   r.scale = scale;
   r.inverse = scale > 0.f ? 1.0 / r.scale : 0.0;
   if (writes) *to = scale;

@@ -118,6 +118,21 @@ def test_norm_q8_special_rows(dtype, d):
             assert torch.isnan(scales).all() and (codes == 0).all()
 
 
+@pytest.mark.parametrize("d", [40000, 8000])
+def test_norm_q8_scales_beyond_fp32(d):
+    """y of up to sqrt(d) times the gain: a scale that fp32 does not hold is NaN, the largest that it holds is right."""
+    x, gain = torch.zeros(2, d), torch.ones(d)
+    x[0, 7], x[1] = 1.0, torch.randn(d, generator=_gen(1))
+    gain[7] = 3e38
+    codes, scales, _ = _norm("rms", x, gain=gain, eps=0.0)
+    _, y = su.norm64("rms", x, None, gain, None, 0.0)
+    if float(y[0].abs().max()) / 127 > torch.finfo(torch.float32).max:
+        assert torch.isnan(scales[0]) and (codes[0] == 0).all()
+    else:
+        su.check_codes(y[:1], codes[:1], scales[:1])
+    su.check_codes(y[1:], codes[1:], scales[1:])
+
+
 def test_norm_q8_ties_go_to_the_even_code():
     """Values in the middle between two codes, with a scale that is no power of two in f32."""
     for dtype, step in (("bf16", 1.0), ("f32", 1.0), ("f32", 0.6875)):
@@ -462,6 +477,51 @@ def test_end_of_a_step_on_another_stream_and_captured():
         captured = [t.clone() for t in end.out]
         end.run()
         assert all(torch.equal(a, b) for a, b in zip(captured, end.out))
+
+
+def test_logprobs_of_few_rows_captured():
+    """A captured call with a workspace of its own, and two graphs that share one, replayed in turn with other logits."""
+    rows, vocab, top = 2, 70001, 4
+    g = _gen(21)
+    x = torch.randn(rows, vocab, generator=g).bfloat16().cuda()
+    tokens = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32).cuda()
+    need = B.dare_k_logprobs_workspace(B.DARE_BF16, rows, vocab, top)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    outs, graphs = [_outputs(rows, top) for _ in range(3)], []
+    B.dare_k_logprobs(x, tokens, *outs[0])
+    torch.cuda.synchronize()
+    for out, w in zip(outs, (None, ws, ws)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            B.dare_k_logprobs(x, tokens, *out, workspace=w)
+    for _ in range(4):
+        x.copy_(torch.randn(rows, vocab, generator=g))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        eager = _outputs(rows, top)
+        B.dare_k_logprobs(x, tokens, *eager)
+        _check(x.cpu(), tokens.cpu(), 1.0, top, eager)
+        for out in outs:
+            assert all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+def test_logprobs_on_two_streams_at_once():
+    rows, vocab, top = 3, 90000, 5
+    g = _gen(22)
+    sets = []
+    for i in range(2):
+        x = torch.randn(rows, vocab, generator=g).bfloat16()
+        tokens = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+        sets.append((x, tokens, x.cuda(), tokens.cuda(), _outputs(rows, top), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, tokens, xd, td, out, stream in sets:
+            B.dare_k_logprobs(xd, td, *out, stream=stream)
+    torch.cuda.synchronize()
+    for x, tokens, xd, td, out, stream in sets:
+        _check(x, tokens, 1.0, top, out)
 
 
 def test_codes_through_a_layer_with_shared_key_heads():
