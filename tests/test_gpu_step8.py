@@ -320,7 +320,7 @@ def test_logprobs_special_rows(dtype, vocab):
     assert (got[0][torch.tensor(keep).cuda()] == -math.inf).all() and torch.isnan(got[0][4:6]).all()
 
 
-@pytest.mark.parametrize("dtype,vocab,lanes", [("bf16", 12000, 256), ("f32", 15001, 256), ("bf16", 126464, 1024), ("f32", 126464, 1024)])
+@pytest.mark.parametrize("dtype,vocab,lanes", [("bf16", 1000, 64), ("f32", 1000, 64), ("bf16", 12000, 256), ("f32", 15001, 256), ("bf16", 126464, 1024), ("f32", 126464, 1024)])
 @pytest.mark.parametrize("top", [1, 7, 32])
 def test_logprobs_largest_logits_in_few_places(dtype, vocab, lanes, top):
     """The largest logits lie in chunks that a few lanes of a workgroup read, in equal and in different values, and more of them than a list of them holds."""
@@ -328,10 +328,11 @@ def test_logprobs_largest_logits_in_few_places(dtype, vocab, lanes, top):
     per = 8 if dtype == "bf16" else 4
     at = torch.arange(vocab) // per % lanes
     x = torch.randn(4, vocab, generator=g).to(TYPES[dtype])
-    x[0, at < 64] = 30.0
-    x[1, at < 40] += 20.0
+    x[0, at < lanes // 4] = 30.0
+    x[1, at < lanes // 6] += 20.0
     x[2] = torch.arange(vocab) / 1000.0
-    x[3], x[3, at < 6 * 64] = -math.inf, (torch.randn(int((at < 6 * 64).sum()), generator=g) * 4).to(TYPES[dtype])
+    few = at < (28 if lanes == 64 else 6 * 64)
+    x[3], x[3, few] = -math.inf, (torch.randn(int(few.sum()), generator=g) * 4).to(TYPES[dtype])
     tokens = torch.zeros(4, dtype=torch.int32)
     got = _outputs(4, top)
     B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got)
@@ -406,11 +407,14 @@ def test_logprobs_special_parts(dtype):
 
 
 def test_logprobs_many_rows_of_few_logits():
-    x = torch.randn(70001, 33, generator=_gen(4)).bfloat16()
-    tokens = torch.randint(0, 33, (70001,), generator=_gen(5), dtype=torch.int32)
-    got = _outputs(70001, 2)
-    B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got)
-    _check(x, tokens, 1.0, 2, got)
+    for rows, vocab, top, dtype in ((70001, 33, 2, "bf16"), (1100, 1023, 32, "f32"), (1024, 4095, 32, "bf16"), (1030, 4001, 5, "f32")):
+        x = torch.randn(rows, vocab, generator=_gen(4)).to(TYPES[dtype])
+        x[3], x[4, 50:], x[5, ::3], x[6] = 1.5, -math.inf, 4.0, -math.inf      # equal ones, few, more than a list holds, none
+        x[7, torch.arange(vocab) // (8 if dtype == "bf16" else 4) % 64 < 20] += 30.0
+        tokens = torch.randint(0, vocab, (rows,), generator=_gen(5), dtype=torch.int32)
+        got = _outputs(rows, top)
+        B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got)
+        _check(x, tokens, 1.0, top, got)
 
 
 # ---- the end of a step ------------------------------------------------------------------------------
