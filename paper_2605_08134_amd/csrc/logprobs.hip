@@ -33,7 +33,7 @@ struct LogprobsDev {
   float* top_logprobs;
   // rows cut into parts of part_len elements: of every part its sums, and the keys of its `top` largest elements, 0 where it has fewer
   int parts, part_len;
-  f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part (WIDE)
+  f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part, 2 where its elements are so low that they do only beside others
   unsigned long long* part_keys;
 };
 
@@ -98,8 +98,8 @@ __device__ __forceinline__ Sums join(Sums a, float c) {
 template <typename T, int THREADS, Does DOES>
 __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs_kernel(LogprobsDev<T> p) {
   constexpr int WAVES = THREADS / 64, E = 16 / sizeof(T);
-  // a wave's largest keys: enough for the k-th largest, and so many that it is near it (of a single wave all)
   constexpr int kListed = THREADS == 64 ? 512 : 2048;  // elements that the list holds
+  // a wave's largest keys: enough for the k-th largest, and so many that it is near it (of a single wave all)
   constexpr int MOST = WAVES == 1 ? 64 : 32 / WAVES > 4 ? 32 / WAVES : 4;
   __shared__ Sums wave_sums[WAVES];
   __shared__ u64 wave_keys[WAVES * MOST], listed[kListed], limit;
@@ -171,8 +171,8 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     for (int k = 0; k < 2; ++k) keys[k] = tid + k * THREADS < n ? p.part_keys[row * n + tid + k * THREADS] : 0;
     // every part has this many keys from its own limit on, so the lowest limit has `top` keys from it on
     if (top > 0 && lane < p.parts) from = p.part_keys[(row * p.parts + lane) * top + (top - 1) / p.parts];
-    if (!__any(part[3] != 0.f)) {
-      all = join<false>(Sums{part[0], part[1], part[2]}, c);
+    all = join<false>(Sums{part[0], part[1], part[2]}, c);
+    if (!__any(part[3] == 1.f || (part[3] == 2.f && all.s == 0.f))) {
       put_sums();
       if (top == 0) return;
       from = over_lanes(from, [](u64 a, u64 b) { return a < b ? a : b; });
@@ -260,20 +260,16 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     if constexpr (WAVES == 1) wave_keys[lane] = key;
     for (int j = 0; WAVES > 1 && j < most; ++j) {
       const float v = over_lanes(left, [](float a, float b) { return fmaxf(a, b); });
-      u64 equal = __ballot(left == v), w = 0;
+      u64 w = 0;
       if (v > -INFINITY) {
-        int owner = __ffsll((long long)equal) - 1;
-        unsigned first = __builtin_amdgcn_readlane(place, owner);
-        while (equal &= equal - 1) {  // the lowest place of equal ones
-          const int l = __ffsll((long long)equal) - 1;
-          const unsigned at = __builtin_amdgcn_readlane(place, l);
-          if (at < first) {
-            first = at;
-            owner = l;
-          }
-        }
+        const u64 equal = __ballot(left == v);
+        unsigned first;
+        if (equal & (equal - 1))  // the lowest place of equal ones
+          first = over_lanes(left == v ? place : ~0u, [](unsigned a, unsigned b) { return a < b ? a : b; });
+        else
+          first = __builtin_amdgcn_readlane(place, __ffsll((long long)equal) - 1);
         w = order_key(v, first);
-        if (lane == owner) left = -INFINITY;
+        if (left == v && place == first) left = -INFINITY;
       }
       if (lane == 0) wave_keys[wave * most + j] = w;
     }
@@ -293,8 +289,14 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
   // no sum: no element, one that is not finite, or a c x beyond fp32
   wide = !(all.s > 0.f);
   if constexpr (DOES == Does::kPart) {
-    if (wide) wide = __syncthreads_or(best > -INFINITY) || undefined();  // (without an element the sums are right)
-    if (tid == 0) p.part_sums[blockIdx.x] = f32x4{all.r, all.s, all.t, wide ? 1.f : 0.f};
+    // (no sum: without an element it is right; c x below fp32, as where the lowest value masks a place, is 0 beside any sum)
+    float says = 0.f;
+    if (wide && (undefined() || all.r > 0.f)) {
+      says = 1.f;
+    } else if (wide) {
+      says = __syncthreads_or(best > -INFINITY) ? 2.f : 0.f;
+    }
+    if (tid == 0) p.part_sums[blockIdx.x] = f32x4{all.r, all.s, all.t, says};
   } else {
     if (wide) {
       __syncthreads();

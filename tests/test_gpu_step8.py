@@ -387,7 +387,7 @@ def test_logprobs_special_parts(dtype):
     """Parts without an element, with NaN or infinity, and with values at the ends of the type, beside ordinary ones."""
     vocab, top = 126464, 5
     lowest = float(torch.finfo(TYPES[dtype]).min)
-    x = torch.randn(8, vocab, generator=_gen(8)).to(TYPES[dtype])
+    x = torch.randn(11, vocab, generator=_gen(8)).to(TYPES[dtype])
     x[0] = -math.inf
     x[1], x[1, 70000] = -math.inf, 2.0
     x[2, 126463] = math.nan
@@ -397,12 +397,15 @@ def test_logprobs_special_parts(dtype):
     x[6, 60000:] = -math.inf
     x[6, :8192] = -math.inf
     x[7, 9] = -lowest
-    tokens = torch.tensor([5, 70000, 1, 1, 3, 4, 9000, 9], dtype=torch.int32)
-    got = _outputs(8, top)
+    x[8], x[8, 50000] = lowest, -math.inf            # one value, but for a place
+    x[9, 20000:], x[9, :10] = lowest, -lowest         # both ends
+    x[10], x[10, 100000:100003] = -math.inf, lowest   # all of the probability on three of the lowest values
+    tokens = torch.tensor([5, 70000, 1, 1, 3, 4, 9000, 9, 50000, 3, 100001], dtype=torch.int32)
+    got = _outputs(11, top)
     B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got)
     for r in (2, 3):
         assert torch.isnan(got[0][r]) and torch.isnan(got[1][r]) and (got[2][r] == -1).all() and torch.isnan(got[3][r]).all()
-    keep = [0, 1, 4, 5, 6, 7]
+    keep = [0, 1, 4, 5, 6, 7, 8, 9, 10]
     _check(x[keep], tokens[keep], 1.0, top, [t[torch.tensor(keep).cuda()] for t in got])
 
 
