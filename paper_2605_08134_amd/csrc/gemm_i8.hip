@@ -61,7 +61,7 @@ struct I8Op {
 #pragma unroll
           for (int e = 0; e < W; ++e) v[e] = activate_f32(p.act, v[e]);
         } else {
-          activate(p.act, v);
+          activate<true>(p.act, v);
         }
         out_t o;
 #pragma unroll

@@ -142,7 +142,9 @@ __device__ __forceinline__ float silu(float g) {
 // programming): evaluated in fp32 the result is off by 7e-7 at most and, where it falls to 0, by 4.7e-4 of itself, an eighth of the rounding to
 // bf16, down to z = -13, where it ends.  (One term more: 1e-7 and 1.3e-4, but 16384 x 12288 x 4096 1225 us for 1212, x 4096 x 512 136 for 130.)
 // Tanh form: z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
-template <int N>
+// MED: minimum and maximum as the middle of three, which saves the instructions that quiet a NaN in front of them (a NaN is in e as well): the same values,
+// 16384 x 12288 x 4096 in 8 bits 712 -> 700 us.
+template <bool MED = false, int N>
 __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
   if (act == DARE_ACT_SILU) {
 #pragma unroll
@@ -156,7 +158,10 @@ __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
       e = fmaf(t, e, 0.024472961f);
       e = fmaf(t, e, 0.16388455f);
       e = fmaf(t, e, 0.13775338f) * t * __builtin_amdgcn_exp2f(-0.72134752f * x * x);
-      v[i] = fmaf(-fminf(x, 1e18f), e, fmaxf(z, 0.f));  // (infinity times 0 is none)
+      if constexpr (MED)
+        v[i] = fmaf(-__builtin_amdgcn_fmed3f(x, 0.f, 1e18f), e, __builtin_amdgcn_fmed3f(z, 0.f, INFINITY));
+      else
+        v[i] = fmaf(-fminf(x, 1e18f), e, fmaxf(z, 0.f));  // (infinity times 0 is none)
     }
   } else if (act == DARE_ACT_GELU_TANH) {
 #pragma unroll
@@ -814,7 +819,7 @@ __device__ __forceinline__ void gemm_tiles_quad(const typename Op::Dev& p, const
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 v[e] = fmaf(value(i, j + h, e) * row_scale[i], col_scale[h][e >> 2][e & 3], (float)bias[h][e]);
-              activate(p.act, v);
+              activate<true>(p.act, v);
               if (p.residual) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += (float)res[i & 1][h][e];

@@ -245,6 +245,26 @@ def test_linear_q8_largest_sums_and_scales_that_are_not_finite(m):
     assert torch.isfinite(out[keep]).all() and (out[0][keep[0]] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [3, 40, 1600])
+def test_linear_q8_special_values_of_activations(dtype, m):
+    """The identity far above 0, 0 far below, infinities of the bias (GELU of -infinity is 0, the others are NaN there), NaN in its column alone."""
+    td = TYPES[dtype]
+    n = 14144 if m > 1000 else 64
+    a, wt = torch.zeros(m, 384, dtype=torch.int8, device="cuda"), torch.zeros(n, 384, dtype=torch.int8, device="cuda")
+    one = lambda k: torch.ones(k, device="cuda")
+    bias = torch.zeros(n, dtype=td, device="cuda")
+    bias[:6] = torch.tensor([200.0, -200.0, 1e30, -1e30, math.inf, math.nan])
+    bias[n - 1] = -math.inf
+    for act in ("silu", "gelu", "gelu_tanh"):
+        out = torch.empty(m, n, dtype=td, device="cuda")
+        B.dare_k_linear_q8(a, one(m), wt, one(n), out, bias, act)
+        assert (out[:, 0] == bias[0]).all() and (out[:, 2] == bias[2]).all() and (out[:, 4] == math.inf).all()
+        assert (out[:, 1].abs() < 1e-30).all() and (out[:, 3].abs() < 1e-30).all() and torch.isnan(out[:, 5]).all()
+        assert (out[:, n - 1] == 0).all() if act == "gelu" else torch.isnan(out[:, n - 1]).all()
+        assert (out[:, 6:n - 1] == 0).all()
+
+
 def test_linear_q8_scales_whose_product_is_no_normal_number():
     a, wt = torch.full((2, 128), 100, dtype=torch.int8, device="cuda"), torch.full((64, 128), 100, dtype=torch.int8, device="cuda")
     sa, sw = torch.full((2,), 1e-20, device="cuda"), torch.full((64,), 3e-20, device="cuda")
