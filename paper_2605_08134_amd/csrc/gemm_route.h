@@ -189,8 +189,8 @@ constexpr GemmRoute linear_route(int m, int n, int k) {
 //   * up to 32 rows of outputs so wide that one round of 64 x 128 is not enough: 32 x 64, two workgroups per CU, of which one multiplies while the other starts or
 //     stores (1 x 126464 x 4096 98 us and 113, 32 x 126464 x 4096 114 and 121, 3 x 71808 x 384 12.4 and 15.0; on the other side 28 x 24128 x 8320 47.1 and 39.1).
 // 64 x 64 has four stages for the same reason, where bf16 has eight (64 x 126464 x 4096 131 -> 123, 92 x 12544 x 512 8.4 -> 6.2, single rounds as they were).
-// Over 287 sizes (1 to 16384 rows, 384 to 126464 columns, k 384 to 12288) the shape taken is on average 0.7 % behind the fastest, at most 12 % (10 x 896 x
-// 640 3.05 and 2.71).
+// Over 337 sizes (1 to 16384 rows, 384 to 126464 columns, k 384 to 12288) the shape taken is on average 0.7 % behind the fastest, at most 23 % (50 x 39744 x
+// 1152 19.0 and, in one round of 128 x 192, 15.4; beyond 33 to 64 rows at most 12 %, 10 x 896 x 640 3.05 and 2.71).
 constexpr GemmRoute linear_q8_route(int m, int n, int k, bool bf16) {
   const bool quad = bf16 && k / kRouteBK >= kQuadMinSteps;
   if (m <= 8 && n <= 4096) return GemmRoute::kSkinny;
