@@ -89,7 +89,7 @@ def logprobs64(x, tokens, scale, top):
 # columns' multiple of 64 leaves nothing ragged
 LINEAR_Q8_SHAPES = [
     ("kSkinny", 5, 448, 8704), ("k32x32", 19, 320, 8320), ("k32x32", 65, 1088, 2048), ("k64x32", 213, 1344, 768), ("k64x64", 65, 4160, 4224),
-    ("k64x64", 2, 8256, 2176), ("k32x64", 1, 126464, 384), ("k32x64", 3, 40000, 128), ("k32x64", 32, 66624, 384), ("k64x96", 65, 8320, 2176),
+    ("k64x64", 2, 8256, 2176), ("k32x64", 1, 126464, 384), ("k32x64", 3, 50048, 128), ("k128x192", 3, 40000, 128), ("k128x192", 61, 46464, 256), ("k32x64", 32, 66624, 384), ("k64x96", 65, 8320, 2176),
     ("k64x96", 650, 1728, 384), ("k64x96", 20, 18944, 128), ("k64x128", 65, 12352, 1152), ("k64x128", 36, 26560, 384), ("k128x96", 130, 11008, 1920),
     ("k128x96", 1287, 1792, 256), ("k128x128", 130, 12352, 1408), ("k128x128", 1024, 4096, 384), ("k128x192", 258, 11008, 2048),
     ("k128x192", 777, 6144, 256), ("kQuad192", 514, 11008, 2048), ("kQuad192", 1026, 13120, 384), ("kQuad192", 877, 9856, 384),
