@@ -324,7 +324,8 @@ dare_status dare_k_linear_q8(const dare_linear_q8_call* call, void* hip_stream);
  * alternatives than top, ids of -1 and log-probabilities of -infinity fill up; a row without any has the entropy 0.  A token outside [0, vocab) has
  * the log-probability -infinity.  A row with NaN or +infinity: NaN, ids -1.
  * Sums in fp32; a log-probability or an entropy is off by a few 2^-23 of 1, of its size and of how far, in scaled logits, the probability lies
- * from the largest one on average.
+ * from the largest one on average, whatever the logits' own size.  (Rows whose largest scaled logit is beyond 5.8e6 are read twice where scale is below
+ * 65536.)
  *   logits [n_rows, ld] dtype, any alignment of an element; tokens [n_rows] int32 with logprobs [n_rows] fp32, or both NULL; entropy [n_rows]
  *   fp32 or NULL; top_ids [n_rows, top] int32, top_logprobs [n_rows, top] fp32
  * workspace: dare_k_logprobs_workspace() bytes (for the same sizes; it does not look at the pointers), 16-byte aligned, needed while the call runs,

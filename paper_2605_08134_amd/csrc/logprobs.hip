@@ -33,7 +33,7 @@ struct LogprobsDev {
   float* top_logprobs;
   // rows cut into parts of part_len elements: of every part its sums, and the keys of its `top` largest elements, 0 where it has fewer
   int parts, part_len;
-  f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part, 2 where its elements are so low that they do only beside others
+  f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part, 2 where they do only beside a part whose r is above kLowest
   unsigned long long* part_keys;
 };
 
@@ -67,11 +67,18 @@ __device__ __forceinline__ u64 wave_max(u64 v) {
   return over_lanes(v, [](u64 a, u64 b) { return a > b ? a : b; });
 }
 
-// Sums of a set of elements in units of 2^r, exponents d = c x - r, c = scale log2(e), by one product and sum each.  r is near the largest of c x, and
-// any r is right: its rounding is in no exponent.  WIDE: r stands for an x and exponents are c (x - r), which takes an instruction more
-// and holds where c x does not (logits near the largest and lowest values of fp32).
+// Sums of a set of elements in units of 2^r, exponents d = c x - r, c = scale log2(e), by one product and sum each, rounded once.  r is c x of the
+// largest element, rounded.  It cancels in every result, so any r near it is right; but the largest element's own exponent is that
+// rounding, up to half a step of r: at most 1/4 where |r| is below 2^23, but 128 and more, beyond fp32 as a power, from 2^31 on.  So
+//   * r is not below kLowest = -2^23.  Elements that far down have exponents below 1/4, or 0 beside any r that is above it.
+//   * A row whose r comes out as -2^23 or 2^23 or beyond (scaled logits beyond 5.8e6: temperatures near 0, or all of the row on a low mask) takes a
+//     second pass.
+// WIDE, the second pass: r stands for an x and exponents are c (x - r), which takes an instruction more and has no such limits.
+// From scales of kWideScale on, where logits of 90 are as much, it is the first and only one (2048 x 126464 at a scale of 1e8: 94 us, 161 with both
+// passes, 92 with the first alone).
+constexpr float kLowest = -8388608.f, kWideScale = 65536.f;
 struct Sums {
-  float r;  // -FLT_MAX without an element
+  float r;  // kLowest or -FLT_MAX (WIDE: -FLT_MAX) without an element
   float s;  // sum of 2^d
   float t;  // sum of 2^d d
 };
@@ -122,7 +129,8 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
   if (tid == 0) n_lanes = n_listed = 0;
 
   Sums all;
-  bool wide = false;
+  const bool wide_first = p.scale >= kWideScale;
+  bool wide = wide_first;
   // (a NaN, or the difference of two infinities, is in the sum)
   auto undefined = [&]() { return !(all.s >= 0.f); };
   auto logprob = [&](float v) {
@@ -171,8 +179,9 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     for (int k = 0; k < 2; ++k) keys[k] = tid + k * THREADS < n ? p.part_keys[row * n + tid + k * THREADS] : 0;
     // every part has this many keys from its own limit on, so the lowest limit has `top` keys from it on
     if (top > 0 && lane < p.parts) from = p.part_keys[(row * p.parts + lane) * top + (top - 1) / p.parts];
-    all = join<false>(Sums{part[0], part[1], part[2]}, c);
-    if (!__any(part[3] == 1.f || (part[3] == 2.f && all.s == 0.f))) {
+    const Sums sums = {part[0], part[1], part[2]};
+    all = wide_first ? join<true>(sums, c) : join<false>(sums, c);
+    if (!__any(part[3] == 1.f || (part[3] == 2.f && all.r == kLowest))) {
       put_sums();
       if (top == 0) return;
       from = over_lanes(from, [](u64 a, u64 b) { return a < b ? a : b; });
@@ -193,7 +202,7 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
   // the row's sums, in wave_sums by waves
   auto pass = [&](auto wide) {
     constexpr bool WIDE = decltype(wide)::value;
-    Sums sum = {-__FLT_MAX__, 0.f, 0.f};
+    Sums sum = {WIDE ? -__FLT_MAX__ : kLowest, 0.f, 0.f};
     auto take = [&](const float (&v)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -252,7 +261,10 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
   auto joined = [&](auto wide) {
     return join<decltype(wide)::value, WAVES == 16 ? 4 : WAVES == 4 ? 2 : 0>(wave_sums[lane % WAVES], c);
   };
-  pass(std::false_type{});
+  if (wide_first)
+    pass(std::true_type{});
+  else
+    pass(std::false_type{});
   u64 key = best > -INFINITY ? order_key(best, place) : 0;
   if (top > 0) {
     const int most = WAVES == 1 ? 64 : (top + WAVES - 1) / WAVES > 4 ? (top + WAVES - 1) / WAVES : top < 4 ? top : 4;
@@ -285,20 +297,21 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     }
   }
   __syncthreads();
-  all = joined(std::false_type{});
-  // no sum: no element, one that is not finite, or a c x beyond fp32
-  wide = !(all.s > 0.f);
+  all = wide_first ? joined(std::true_type{}) : joined(std::false_type{});
+  // r too large (or infinite) for the sums; or too low, which it also is without an element; or an element that is NaN
+  const bool again = !wide_first && (!(fabsf(all.r) < -kLowest) || undefined());
   if constexpr (DOES == Does::kPart) {
-    // (no sum: without an element it is right; c x below fp32, as where the lowest value masks a place, is 0 beside any sum)
+    // (too low, as where a number masks all places: right beside a part that is not; without an element: right)
     float says = 0.f;
-    if (wide && (undefined() || all.r > 0.f)) {
+    if (again && (undefined() || all.r > 0.f)) {
       says = 1.f;
-    } else if (wide) {
+    } else if (again) {
       says = __syncthreads_or(best > -INFINITY) ? 2.f : 0.f;
     }
     if (tid == 0) p.part_sums[blockIdx.x] = f32x4{all.r, all.s, all.t, says};
   } else {
-    if (wide) {
+    if (again) {
+      wide = true;
       __syncthreads();
       pass(std::true_type{});
       __syncthreads();
