@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     if (undefined()) return __builtin_nanf("");
     if (v == -INFINITY) return -INFINITY;
     const float log2_sum = __log2f(all.s);
-    if (wide) return (v - all.r) * p.scale - kLn2 * log2_sum;
+    if (wide) return 2.f * ((0.5f * v - 0.5f * all.r) * p.scale) - kLn2 * log2_sum;  // (the difference may be beyond fp32, times scale it need not)
     const float d = fmaf(v, c, -all.r) - log2_sum;
     return d > -INFINITY ? kLn2 * d : fmaf(v, p.scale, -kLn2 * all.r);  // (c v beyond fp32, scale v perhaps not)
   };

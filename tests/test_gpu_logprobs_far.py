@@ -111,3 +111,18 @@ def test_logprobs_of_masked_parts(dtype, mask, scale):
     for r in (6, 7, 8):
         assert torch.isnan(got[0][r]) and torch.isnan(got[1][r]) and (got[2][r] == -1).all() and torch.isnan(got[3][r]).all()
     _check(x[:6], tokens[:6], scale, top, [t[:6] for t in got])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5, 1000, 40000, 126464])
+@pytest.mark.parametrize("scale", [1e-31, 1e-3, 0.3, 0.49, 0.6, 0.7])
+def test_logprobs_of_differences_beyond_fp32(dtype, vocab, scale):
+    """A largest logit near the type's end: a lower one's distance from it is beyond fp32, times the scale it is not."""
+    most = float(torch.finfo(TYPES[dtype]).max)
+    x = torch.zeros(6, vocab, dtype=TYPES[dtype])
+    for r, v in enumerate((-1e37, -1e36, -0.4 * most, -0.9 * most, -most, 1e37)):
+        x[r], x[r, 1] = v, most
+        x[r, 2::7] = -v / 3
+    x[5, 3] = -most
+    tokens = torch.tensor([0, 0, 0, 0, 4, 3], dtype=torch.int32)
+    _run(x, tokens, scale, 5)
