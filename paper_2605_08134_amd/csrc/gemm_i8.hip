@@ -63,9 +63,9 @@ struct I8Op {
         } else {
           activate<true>(p.act, v);
         }
-        out_t o;
+        out_t o;  // (a sum with -0 has all bits of the other term: an activation's -0 stays, as in the wide tiles, which add nothing)
 #pragma unroll
-        for (int e = 0; e < W; ++e) o[e] = (T)(v[e] + (residual ? (float)res[i][e] : 0.f));
+        for (int e = 0; e < W; ++e) o[e] = (T)(v[e] + (residual ? (float)res[i][e] : -0.f));
         if (live[i]) *reinterpret_cast<out_t*>(out + tok[i] * ldc + c) = o;
       }
     }

@@ -97,3 +97,11 @@ LINEAR_Q8_SHAPES = [
     ("kQuad256", 770, 12352, 8320),      # one round of tiles, a long k
     ("kQuad256", 4617, 15424, 384),      # more than 128 MB of outputs, which are stored past the L2
 ]
+
+# (columns, k, numbers of rows): calls whose common rows have the same bits although their tiles have other shapes; together every shape there is
+LINEAR_Q8_ROWS = [
+    (4096, 384, (5, 9, 70, 140, 260, 330, 520, 650, 1030, 1420)),
+    (12352, 384, (3, 70, 140, 260, 390, 770)),
+    (15424, 384, (5, 300, 4617)),        # the last one stored past the L2
+    (66624, 384, (3, 40, 259)),
+]

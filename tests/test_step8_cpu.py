@@ -180,3 +180,16 @@ def test_shapes_that_the_gpu_tests_name(tmp_path):
     got = subprocess.run([str(tmp_path / "names")], capture_output=True, text=True, check=True).stdout.split()
     assert got == ["1"] * len(su.LINEAR_Q8_SHAPES)
     assert len({s[0] for s in su.LINEAR_Q8_SHAPES}) == 12
+
+
+def test_rows_that_are_compared_are_in_every_shape(tmp_path):
+    src = '#include <cstdio>\n#include "gemm_route.h"\nusing namespace dare;\nint main() {\n'
+    calls = [(n, k, m) for n, k, rows in su.LINEAR_Q8_ROWS for m in rows]
+    for n, k, m in calls:
+        src += "  std::printf(\"%%d %%d \", (int)linear_q8_route(%d, %d, %d, true), (int)linear_q8_route(%d, %d, %d, false));\n" % (2 * (m, n, k // 2))
+    (tmp_path / "rows.cpp").write_text(src + "}\n")
+    csrc = os.path.join(ROOT, "paper_2605_08134_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "rows.cpp"), "-o", str(tmp_path / "rows")], check=True)
+    got = subprocess.run([str(tmp_path / "rows")], capture_output=True, text=True, check=True).stdout.split()
+    assert len(got) == 2 * len(calls)
+    assert len(set(got[0::2])) == 12 and len(set(got[1::2])) == 10       # (two shapes are there for bf16 outputs only)
