@@ -551,7 +551,7 @@ _PACKED_CALL = struct.Struct("@I10if4q7P")
 def _pack(layout, *fields):
     try:
         return layout.pack(layout.size, *fields)
-    except (struct.error, OverflowError) as e:   # (a float beyond fp32 is the latter)
+    except struct.error as e:
         raise ValueError("an argument does not fit its type: %s" % e) from None
 
 

@@ -193,9 +193,3 @@ def test_rows_that_are_compared_are_in_every_shape(tmp_path):
     got = subprocess.run([str(tmp_path / "rows")], capture_output=True, text=True, check=True).stdout.split()
     assert len(got) == 2 * len(calls)
     assert len(set(got[0::2])) == 12 and len(set(got[1::2])) == 10       # (two shapes are there for bf16 outputs only)
-
-
-@pytest.mark.parametrize("scale", [1e39, -1e300, "1", None])
-def test_scale_that_is_no_fp32_number_is_a_value_error(scale):
-    with pytest.raises(ValueError):
-        B._pack(B._LOGPROBS_CALL, B.DARE_F32, 1, 100, 0, scale, 100, *[0] * 6)
