@@ -261,24 +261,26 @@ dare_status dare_k_attention_packed_workspace(const dare_packed_call* call, size
 dare_status dare_k_attention_packed(const dare_packed_call* call, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
- * Operators of a step in 8 bits and of its output end: normalisation into codes, projection of codes, and what decides from logits which
- * positions to unmask.  Sizes of 0 rows are fine (nothing is enqueued), every ld is the distance of two rows in elements, nothing is allocated
- * and nothing kept.  dare_last_error(NULL) has the text of a refusal.
+ * Operators of a step in 8 bits and of its output end: normalisation into codes, projection of codes, and what decides
+ * from logits which positions to unmask.  Sizes of 0 rows are fine (nothing is enqueued), every ld is the distance of
+ * two rows in elements, nothing is allocated and nothing kept.  dare_last_error(NULL) has the text of a refusal.
  *
  * Normalisation of token rows into 8-bit codes with a scale per row, behind the residual sum.  For row t of d channels
  *     s = x[t] + o[t], rounded to dtype (x[t] without o); x_out[t] = s
  *     y = s | (s - mean) / sqrt(var + eps) * gain + bias | s / sqrt(mean(s^2) + eps) * gain     (DARE_NORM_NONE | LAYER | RMS)
  *     scales[t] = max |y| / 127 rounded to fp32,  codes[t] = y / scales[t] to the nearest whole number, ties to even, in [-127, 127]
- * so that codes[t] * scales[t] stands for y.  Sums, y and the decision between two codes are formed in 64 bits.  A row of zeros has the scale 0
- * and codes 0; one with a value that is not finite (zeros under DARE_NORM_RMS with eps 0 are), or with a scale beyond fp32, the scale NaN and codes 0, and its
- * projections are NaN.
+ * so that codes[t] * scales[t] stands for y.  Sums, y and the decision between two codes are formed in 64 bits.  A row
+ * of zeros has the scale 0 and codes 0; one with a value that is not finite (zeros under DARE_NORM_RMS with eps 0 are),
+ * or with a scale beyond fp32, the scale NaN and codes 0, and its projections are NaN.
  * The codes of a weight: DARE_NORM_NONE of the rows of the packed matrix (dare_k_pack_weight), one scale per output column.
- *   x, o, x_out  [n_rows, ldx | ldo | ldxo] dtype on 16-byte boundaries; o and x_out may be NULL; x_out may be x or o (with the same ld)
+ *   x, o, x_out  [n_rows, ldx | ldo | ldxo] dtype on 16-byte boundaries; o and x_out may be NULL; x_out may be x or o
+ *                (with the same ld)
  *   gain, bias   [d] dtype on 16-byte boundaries; gain for both norms, bias (or NULL) for LAYER
  *   codes        [n_rows, ldc], on 8-byte boundaries          scales [n_rows]
  * There is no other overlap.  d is a multiple of 8.
- * Errors: INVALID_ARG (struct_size, null pointer, unknown dtype or kind, sizes, eps, ld below the row's width, alignment, a gain or bias that the
- * kind does not have), UNSUPPORTED (d not a multiple of 8 or beyond 2^24, n_rows beyond 2^23, an ld beyond 2^24).
+ * Errors: INVALID_ARG (struct_size, null pointer, unknown dtype or kind, sizes, eps, ld below the row's width,
+ * alignment, a gain or bias that the kind does not have), UNSUPPORTED (d not a multiple of 8 or beyond 2^24, n_rows
+ * beyond 2^23, an ld beyond 2^24).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_norm_q8_call) */
@@ -295,13 +297,14 @@ dare_status dare_k_norm_q8(const dare_norm_q8_call* call, void* hip_stream);
 /*
  * Projection of 8-bit codes with scales for each row and each column:
  *     out[t, c] = act(row_scale[t] col_scale[c] sum_k a[t, k] wt[c, k] + bias[c]) + residual[t, c]      for t in [0, m), c in [0, n)
- * The sum is exact, in 32-bit integers (codes -128 .. 127); scales, bias, activation (as in dare_k_linear) and residual sum in fp32, one rounding
- * to dtype, the type of bias, residual and out.
+ * The sum is exact, in 32-bit integers (codes -128 .. 127); scales, bias, activation (as in dare_k_linear) and residual
+ * sum in fp32, one rounding to dtype, the type of bias, residual and out.
  *   a [m, lda], wt [n, k] codes and col_scale [n] on 16-byte boundaries; row_scale [m]
  *   bias [n] or NULL, residual [m, ldr] or NULL, out [m, ldo] dtype on 16-byte boundaries
  * out may be residual (with the same ld); there is no other overlap.  n is a multiple of 64, k of 128.
- * Errors: INVALID_ARG (struct_size, null pointer, sizes, ld below the row's width, alignment, unknown dtype or act), UNSUPPORTED (n not a multiple
- * of 64, k not of 128, k of 2^17 and more, m beyond 2^24, n beyond 2^20, m n beyond 2^37, an ld beyond 2^24).
+ * Errors: INVALID_ARG (struct_size, null pointer, sizes, ld below the row's width, alignment, unknown dtype or act),
+ * UNSUPPORTED (n not a multiple of 64, k not of 128, k of 2^17 and more, m beyond 2^24, n beyond 2^20, m n beyond 2^37,
+ * an ld beyond 2^24).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_linear_q8_call) */
@@ -320,19 +323,22 @@ dare_status dare_k_linear_q8(const dare_linear_q8_call* call, void* hip_stream);
  * Log-probabilities of given tokens, entropy and the largest alternatives of rows of logits, p = softmax(scale logits[t, 0:vocab]):
  *     logprobs[t] = log p[tokens[t]],  entropy[t] = - sum p log p,
  *     top_ids[t, i], top_logprobs[t, i]: the i-th largest logit's id and log p, of equal logits the lower id first
- * A logit of -infinity has the probability 0: its log-probability is -infinity, it adds nothing to the entropy and is no alternative.  Where a row has fewer
- * alternatives than top, ids of -1 and log-probabilities of -infinity fill up; a row without any has the entropy 0.  A token outside [0, vocab) has
- * the log-probability -infinity.  A row with NaN or +infinity: NaN, ids -1.
- * Sums in fp32; a log-probability or an entropy is off by a few 2^-23 of 1, of its size and of how far, in scaled logits, the probability lies
- * from the largest one on average, whatever the logits' own size.  (Rows whose largest scaled logit is beyond 5.8e6 are read twice where scale is below
- * 65536.)
- *   logits [n_rows, ld] dtype, any alignment of an element; tokens [n_rows] int32 with logprobs [n_rows] fp32, or both NULL; entropy [n_rows]
- *   fp32 or NULL; top_ids [n_rows, top] int32, top_logprobs [n_rows, top] fp32
- * workspace: dare_k_logprobs_workspace() bytes (for the same sizes; it does not look at the pointers), 16-byte aligned, needed while the call runs,
- * not initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
+ * A logit of -infinity has the probability 0: its log-probability is -infinity, it adds nothing to the entropy and is
+ * no alternative.  Where a row has fewer alternatives than top, ids of -1 and log-probabilities of -infinity fill up; a
+ * row without any has the entropy 0.  A token outside [0, vocab) has the log-probability -infinity.  A row with NaN or
+ * +infinity: NaN, ids -1.
+ * Sums in fp32, of max(64, vocab / 256) terms in a row at most; a log-probability or an entropy is off by a few 2^-23
+ * of 1, of its size and of how far, in scaled logits, the probability lies from the largest one on average, whatever
+ * the logits' own size, and by what the roundings of such a sum may add.  (Rows whose largest scaled logit is beyond
+ * 5.8e6 are read twice where scale is below 65536.)
+ *   logits [n_rows, ld] dtype, any alignment of an element; tokens [n_rows] int32 with logprobs [n_rows] fp32, or both
+ *   NULL; entropy [n_rows] fp32 or NULL; top_ids [n_rows, top] int32, top_logprobs [n_rows, top] fp32
+ * workspace: dare_k_logprobs_workspace() bytes (for the same sizes; it does not look at the pointers), 16-byte aligned,
+ * needed while the call runs, not initialised and not kept; NULL if that is 0.  Calls that may overlap need one each.
  * Nothing overlaps.  top is 0 .. 32 and at most vocab; scale (1 / temperature) above 0, at most 1e30.
- * Errors: INVALID_ARG (struct_size, null pointer, unknown dtype, sizes, scale, ld below vocab, alignment, tokens without logprobs or the other
- * way round, workspace too small), UNSUPPORTED (top above 32, n_rows beyond 2^21, vocab beyond 2^28, ld beyond 2^32).
+ * Errors: INVALID_ARG (struct_size, null pointer, unknown dtype, sizes, scale, ld below vocab, alignment, tokens
+ * without logprobs or the other way round, workspace too small), UNSUPPORTED (top above 32, n_rows beyond 2^21, vocab
+ * beyond 2^28, ld beyond 2^32).
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(dare_logprobs_call) */

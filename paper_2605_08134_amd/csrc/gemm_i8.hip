@@ -1,12 +1,12 @@
 // Projection of 8-bit codes on the gfx950 matrix cores:
 //     out[t, c] = act(row_scale[t] col_scale[c] sum_k A[t, k] W[c, k] + bias[c]) + residual[t, c]
 //
-// The sum is formed in 32-bit integers, so it is exact (k below 2^17: 128 * 128 * k < 2^31) whatever its order: a row's result does not depend on the
-// shape of the tile it is computed in.  It is rounded to fp32 once and scaled there, by the row first; bias, activation
-// and residual sum in fp32, one rounding to the output's type.
+// The sum is formed in 32-bit integers, so it is exact (k below 2^17: 128 * 128 * k < 2^31) whatever its order: a row's
+// result does not depend on the shape of the tile it is computed in.  It is rounded to fp32 once and scaled there, by
+// the row first; bias, activation and residual sum in fp32, one rounding to the output's type.
 //
-// Tiles, LDS layout and loops are those of the bf16 projection (gemm_tiles.h): v_mfma_i32_16x16x64_i8 takes the bytes and the time of
-// v_mfma_f32_16x16x32_bf16 and twice the k, so k codes cost what k / 2 bf16 do.
+// Tiles, LDS layout and loops are those of the bf16 projection (gemm_tiles.h): v_mfma_i32_16x16x64_i8 takes the bytes
+// and the time of v_mfma_f32_16x16x32_bf16 and twice the k, so k codes cost what k / 2 bf16 do.
 #include "gemm_tiles.h"
 
 namespace dare {

@@ -179,20 +179,25 @@ constexpr GemmRoute linear_route(int m, int n, int k) {
   return gemm_route(m, n, k, 1, false);
 }
 
-// 8-bit codes (k in units of two): what a shape costs in bytes and cycles per k-step is what it costs in bf16, so the costs are those of best_tile, the
-// wide tiles in their four-wave form (quad_cost), which is there for bf16 outputs and three k-steps.  A sum has half as many k-steps, starts and ends
-// weigh twice as much, and few rows want more and smaller workgroups than in bf16:
-//   * up to 8 rows of up to 4096 columns, one workgroup per 16 columns on the 256 CUs: the stream over the weights (us, it and 32 x 32: 1 x 4096 x 4096 6.7
-//     7.3, 8 x 1024 x 512 2.7 2.9; on the other side 5 x 4416 x 4352 11.0 7.7, 16 x 4096 x 4096 8.2 8.1);
-//   * as long as one round is enough for them, 32 x 32, then 64 x 32, then 64 x 64 (64 x 4096 x 12288 19.7, 26.9 and more, 105 x 3648 x 6272 14.7 14.4 17.2, 143 x 3648
-//     x 2048 8.9 8.7 7.3);
-//   * up to 64 rows of outputs that 64 x 128 need a second round for and 128 x 192 do not: these (50 x 39744 x 1152 15.4 and 19.0, 43 x 48960 x 8064 71.3 and 82.4, 64 x 46464
-//     x 4352 42.9 and 48.9, 7 x 48576 x 1280 16.0 and 17.3, but 3 x 46272 x 2176 21.8 and 20.8);
-//   * up to 32 rows of outputs so wide that one round of 64 x 128 is not enough: 32 x 64, two workgroups per CU, of which one multiplies while the other starts or
-//     stores (1 x 126464 x 4096 98 us and 113, 32 x 126464 x 4096 114 and 121, 3 x 71808 x 384 12.4 and 15.0; on the other side 28 x 24128 x 8320 47.1 and 39.1).
-// 64 x 64 has four stages for the same reason, where bf16 has eight (64 x 126464 x 4096 131 -> 123, 92 x 12544 x 512 8.4 -> 6.2, single rounds as they were).
-// Over 337 sizes (1 to 16384 rows, 384 to 126464 columns, k 384 to 12288) the shape taken is on average 0.6 % behind the fastest, at most 12 % (10 x 896 x
-// 640 3.05 and 2.71, 52 x 101824 x 768 31.5 and 28.1).
+// 8-bit codes (k in units of two): what a shape costs in bytes and cycles per k-step is what it costs in bf16, so the
+// costs are those of best_tile, the wide tiles in their four-wave form (quad_cost), which is there for bf16 outputs and
+// three k-steps.  A sum has half as many k-steps, starts and ends weigh twice as much, and few rows want more and
+// smaller workgroups than in bf16:
+//   * up to 8 rows of up to 4096 columns, one workgroup per 16 columns on the 256 CUs: the stream over the weights (us,
+//     it and 32 x 32: 1 x 4096 x 4096 6.7 7.3, 8 x 1024 x 512 2.7 2.9; on the other side 5 x 4416 x 4352 11.0 7.7, 16 x
+//     4096 x 4096 8.2 8.1);
+//   * as long as one round is enough for them, 32 x 32, then 64 x 32, then 64 x 64 (64 x 4096 x 12288 19.7, 26.9 and
+//     more, 105 x 3648 x 6272 14.7 14.4 17.2, 143 x 3648 x 2048 8.9 8.7 7.3);
+//   * up to 64 rows of outputs that 64 x 128 need a second round for and 128 x 192 do not: these (50 x 39744 x 1152
+//     15.4 and 19.0, 43 x 48960 x 8064 71.3 and 82.4, 64 x 46464 x 4352 42.9 and 48.9, 7 x 48576 x 1280 16.0 and 17.3,
+//     but 3 x 46272 x 2176 21.8 and 20.8);
+//   * up to 32 rows of outputs so wide that one round of 64 x 128 is not enough: 32 x 64, two workgroups per CU, of
+//     which one multiplies while the other starts or stores (1 x 126464 x 4096 98 us and 113, 32 x 126464 x 4096 114
+//     and 121, 3 x 71808 x 384 12.4 and 15.0; on the other side 28 x 24128 x 8320 47.1 and 39.1).
+// 64 x 64 has four stages for the same reason, where bf16 has eight (64 x 126464 x 4096 131 -> 123, 92 x 12544 x 512
+// 8.4 -> 6.2, single rounds as they were).  Over 337 sizes (1 to 16384 rows, 384 to 126464 columns, k 384 to 12288) the
+// shape taken is on average 0.6 % behind the fastest, at most 12 % (10 x 896 x 640 3.05 and 2.71, 52 x 101824 x 768
+// 31.5 and 28.1).
 constexpr GemmRoute linear_q8_route(int m, int n, int k, bool bf16) {
   const bool quad = bf16 && k / kRouteBK >= kQuadMinSteps;
   if (m <= 8 && n <= 4096) return GemmRoute::kSkinny;

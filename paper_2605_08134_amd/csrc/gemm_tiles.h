@@ -142,8 +142,8 @@ __device__ __forceinline__ float silu(float g) {
 // programming): evaluated in fp32 the result is off by 7e-7 at most and, where it falls to 0, by 4.7e-4 of itself, an eighth of the rounding to
 // bf16, down to z = -13, where it ends.  (One term more: 1e-7 and 1.3e-4, but 16384 x 12288 x 4096 1225 us for 1212, x 4096 x 512 136 for 130.)
 // Tanh form: z / (1 + e^-2y), y = sqrt(2 / pi) (z + 0.044715 z^3).
-// MED: minimum and maximum as the middle of three, which saves the instructions that quiet a NaN in front of them (a NaN is in e as well): the same values,
-// 16384 x 12288 x 4096 in 8 bits 712 -> 700 us.
+// MED: minimum and maximum as the middle of three, which saves the instructions that quiet a NaN in front of them (a
+// NaN is in e as well): the same values, 16384 x 12288 x 4096 in 8 bits 712 -> 700 us.
 template <bool MED = false, int N>
 __device__ __forceinline__ void activate(const int act, float (&v)[N]) {
   if (act == DARE_ACT_SILU) {

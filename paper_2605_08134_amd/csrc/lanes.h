@@ -1,5 +1,5 @@
-// Reductions over the 64 lanes of a wave whose result every lane gets, by the vector unit alone: an exchange through LDS (which a general
-// shuffle is) takes a wave over a hundred cycles, six of them in a row for each value.
+// Reductions over the 64 lanes of a wave whose result every lane gets, by the vector unit alone: an exchange through
+// LDS (which a general shuffle is) takes a wave over a hundred cycles, six of them in a row for each value.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -7,8 +7,9 @@
 namespace dare {
 namespace {
 
-// Step s of 0 .. 5: the words `v` of two groups of 2^s lanes, in all lanes of both.  Within a group every lane holds the same result by then, so it
-// does not matter which lane of the other group is read: neighbours, pairs, half rows and rows of 16 by DPP, the rest by swaps of rows.
+// Step s of 0 .. 5: the words `v` of two groups of 2^s lanes, in all lanes of both.  Within a group every lane holds
+// the same result by then, so it does not matter which lane of the other group is read: neighbours, pairs, half rows
+// and rows of 16 by DPP, the rest by swaps of rows.
 template <int STEP>
 __device__ __forceinline__ void both_halves(unsigned v, unsigned& a, unsigned& b) {
   if constexpr (STEP < 4) {

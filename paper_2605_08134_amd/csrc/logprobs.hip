@@ -1,15 +1,18 @@
 // Log-probabilities of given tokens, entropy and top alternatives of rows of logits x, z = scale x:
 //     S = sum exp(z - r),  logprob(v) = z_v - r - log S,  entropy = log S - sum exp(z - r) (z - r) / S,   r about max z
 //
-// One workgroup per row and one pass over it, bound by memory (exponentials: 64 elements take a SIMD 45 cycles, which is 7 TB/s for bf16).
-// Every lane keeps the sums over its elements relative to its own largest one; they are joined at the end.
+// One workgroup per row and one pass over it, bound by memory (exponentials: 64 elements take a SIMD 45 cycles, which
+// is 7 TB/s for bf16).  Every lane keeps the sums over its elements relative to its own largest one; they are joined at
+// the end.
 //
-// Alternatives.  Order: the larger logit first, of equal ones the lower id; as whole numbers, `order_key`, in which no two elements are equal.
-// In the pass a lane keeps only its largest chunk (16 bytes) and where that lies.  Take T, the k-th largest of the lanes' keys, or a lower one:
-// an element below T has k better ones, so the alternatives lie in the lanes whose key is T or more, about k of them; those lanes' elements are
-// read again (k / 1024 of the row), the ones from T on are listed, and a listed element's rank is how many others are above it.
-// Few rows: parts of a row by a workgroup each, and a second launch that joins what they found.
-// The list may overflow where many of the largest logits fall into the same few lanes; then the alternatives are found one after the other.
+// Alternatives.  Order: the larger logit first, of equal ones the lower id; as whole numbers, `order_key`, in which no
+// two elements are equal.  In the pass a lane keeps only its largest chunk (16 bytes) and where that lies.  Take T, the
+// k-th largest of the lanes' keys, or a lower one: an element below T has k better ones, so the alternatives lie in the
+// lanes whose key is T or more, about k of them; those lanes' elements are read again (k / 1024 of the row), the ones
+// from T on are listed, and a listed element's rank is how many others are above it.  Few rows: parts of a row by a
+// workgroup each, and a second launch that joins what they found.
+// The list may overflow where many of the largest logits fall into the same few lanes; then the alternatives are found
+// one after the other.
 #include <type_traits>
 
 #include "dare_common.h"
@@ -31,7 +34,8 @@ struct LogprobsDev {
   float* entropy;
   int32_t* top_ids;
   float* top_logprobs;
-  // rows cut into parts of part_len elements: of every part its sums, and the keys of its `top` largest elements, 0 where it has fewer
+  // rows cut into parts of part_len elements: of every part its sums, and the keys of its `top` largest elements, 0
+  // where it has fewer
   int parts, part_len;
   f32x4* part_sums;  // (r, s, t), and 1 where they do not stand for the part, 2 where they do only beside a part whose r is above kLowest
   unsigned long long* part_keys;
@@ -67,15 +71,16 @@ __device__ __forceinline__ u64 wave_max(u64 v) {
   return over_lanes(v, [](u64 a, u64 b) { return a > b ? a : b; });
 }
 
-// Sums of a set of elements in units of 2^r, exponents d = c x - r, c = scale log2(e), by one product and sum each, rounded once.  r is c x of the
-// largest element, rounded.  It cancels in every result, so any r near it is right; but the largest element's own exponent is that
-// rounding, up to half a step of r: at most 1/4 where |r| is below 2^23, but 128 and more, beyond fp32 as a power, from 2^31 on.  So
+// Sums of a set of elements in units of 2^r, exponents d = c x - r, c = scale log2(e), by one product and sum each,
+// rounded once.  r is c x of the largest element, rounded.  It cancels in every result, so any r near it is right; but
+// the largest element's own exponent is that rounding, up to half a step of r: at most 1/4 where |r| is below 2^23, but
+// 128 and more, beyond fp32 as a power, from 2^31 on.  So
 //   * r is not below kLowest = -2^23.  Elements that far down have exponents below 1/4, or 0 beside any r that is above it.
-//   * A row whose r comes out as -2^23 or 2^23 or beyond (scaled logits beyond 5.8e6: temperatures near 0, or all of the row on a low mask) takes a
-//     second pass.
-// WIDE, the second pass: r stands for an x and exponents are c (x - r), which takes an instruction more and has no such limits.
-// From scales of kWideScale on, where logits of 90 are as much, it is the first and only one (2048 x 126464 at a scale of 1e8: 94 us, 161 with both
-// passes, 92 with the first alone).
+//   * A row whose r comes out as -2^23 or 2^23 or beyond (scaled logits beyond 5.8e6: temperatures near 0, or all of
+//     the row on a low mask) takes a second pass.
+// WIDE, the second pass: r stands for an x and exponents are c (x - r), which takes an instruction more and has no such
+// limits.  From scales of kWideScale on, where logits of 90 are as much, it is the first and only one (2048 x 126464 at
+// a scale of 1e8: 94 us, 161 with both passes, 92 with the first alone).
 constexpr float kLowest = -8388608.f, kWideScale = 65536.f;
 struct Sums {
   float r;  // kLowest or -FLT_MAX (WIDE: -FLT_MAX) without an element
@@ -213,8 +218,9 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
     };
     auto rise = [&]() { raise<WIDE>(sum, fmaxf(sum.r, WIDE ? best : best * c), c); };
     for (int i = tid; i < chunks; i += kAhead * THREADS) {
-      // Chunks that no lane of the wave has are left out of the arithmetic: bf16, 4096 x 4096 20.1 -> 18.8 us, 1000 x 151936 62.6 -> 60.9; in fp32, with half as much
-      // of it per byte, 300 x 32003 16.5 and 16.6, 1024 x 126464 93.8 and 95.0.
+      // Chunks that no lane of the wave has are left out of the arithmetic: bf16, 4096 x 4096 20.1 -> 18.8 us, 1000 x
+      // 151936 62.6 -> 60.9; in fp32, with half as much of it per byte, 300 x 32003 16.5 and 16.6, 1024 x 126464 93.8
+      // and 95.0.
       constexpr bool kLeaveOut = sizeof(T) == 2;
       const int first = __builtin_amdgcn_readfirstlane(i);
       u32x4 r[kAhead];
@@ -372,9 +378,10 @@ __global__ void __launch_bounds__(THREADS, DOES == Does::kJoin ? 4 : 8) logprobs
   }
 }
 
-// Few rows are cut so that their parts give every CU a workgroup, into pieces that a workgroup loads at once.  One workgroup takes 126464 logits at 16
-// a ns, a part of 8192 costs it 2 us, and the second launch 3 to 5 (us, bf16, uncut and cut: 1 x 126464 with 2 alternatives 12.5 8.2, with 32
-// 14.4 12.9, 32 x 126464 with 8 14.8 11.3, 64 x 126464 in four parts 14.9 13.7, in three 85 x 126464 16.0 16.7; 1 x 32768 6.5 7.4).
+// Few rows are cut so that their parts give every CU a workgroup, into pieces that a workgroup loads at once.  One
+// workgroup takes 126464 logits at 16 a ns, a part of 8192 costs it 2 us, and the second launch 3 to 5 (us, bf16, uncut
+// and cut: 1 x 126464 with 2 alternatives 12.5 8.2, with 32 14.4 12.9, 32 x 126464 with 8 14.8 11.3, 64 x 126464 in
+// four parts 14.9 13.7, in three 85 x 126464 16.0 16.7; 1 x 32768 6.5 7.4).
 int logprobs_parts(int rows, int vocab) {
   if (vocab < 65536) return 1;
   int n = 256 / rows < vocab / 8192 ? 256 / rows : vocab / 8192;
@@ -409,8 +416,9 @@ hipError_t launch(const LogprobsArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((logprobs_kernel<T, 256, Does::kJoin>), dim3(a.rows), dim3(256), 0, s, p);
   } else if (a.vocab < 1024 || (a.vocab < 4096 && a.rows >= 1024)) {
-    // a wave: what a row costs beside its elements is four times less than with four waves, its elements take longer (us, it and four waves: 4096 x 300
-    // 8.1 13.4, 4096 x 1000 8.3 13.8, 4096 x 4000 15.3 19.9, 70000 x 33 61 167; 1 x 1000 4.7 4.6, 1 x 4000 6.7 5.5, 300 x 4000 8.0 6.8)
+    // a wave: what a row costs beside its elements is four times less than with four waves, its elements take longer
+    // (us, it and four waves: 4096 x 300 8.1 13.4, 4096 x 1000 8.3 13.8, 4096 x 4000 15.3 19.9, 70000 x 33 61 167; 1 x
+    // 1000 4.7 4.6, 1 x 4000 6.7 5.5, 300 x 4000 8.0 6.8)
     hipLaunchKernelGGL((logprobs_kernel<T, 64, Does::kRow>), dim3(a.rows), dim3(64), 0, s, p);
   } else if (a.vocab < 16384) {
     hipLaunchKernelGGL((logprobs_kernel<T, 256, Does::kRow>), dim3(a.rows), dim3(256), 0, s, p);

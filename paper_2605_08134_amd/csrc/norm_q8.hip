@@ -2,12 +2,13 @@
 //     s = x + o, rounded to the type and stored;   y = s | LayerNorm(s) | s / sqrt(mean(s^2) + eps) * gain
 //     scale = max |y| / 127 rounded to fp32;       code = y / scale to the nearest whole number, ties to even
 //
-// Everything behind s is formed in 64 bits: a code is the one that the formula has.  In fp32 y / scale is off by up to 127 * 4 * 2^-24 =
-// 3e-5, and a row's codes would hang on the order in which its sum of squares was formed: one code in 10^5 goes to a neighbour, and
-// no other program could say which.
+// Everything behind s is formed in 64 bits: a code is the one that the formula has.  In fp32 y / scale is off by up to
+// 127 * 4 * 2^-24 = 3e-5, and a row's codes would hang on the order in which its sum of squares was formed: one code in
+// 10^5 goes to a neighbour, and no other program could say which.
 //
-// Memory-bound: one read of x and o, one write of s and of a byte per channel.  A row is held in registers from its load to its codes, by
-// 8 to 64 lanes (rows of up to 1024 channels) or a workgroup of four waves (up to 16384); longer rows are read once per pass.
+// Memory-bound: one read of x and o, one write of s and of a byte per channel.  A row is held in registers from its
+// load to its codes, by 8 to 64 lanes (rows of up to 1024 channels) or a workgroup of four waves (up to 16384); longer
+// rows are read once per pass.
 #include <type_traits>
 
 #include "dare_common.h"
@@ -106,8 +107,9 @@ __device__ __forceinline__ RowScale row_scale(double largest, double rest, float
   return r;
 }
 
-// Rows of up to 8 LANES HOLD channels, LANES to a row.  y is held from the statistic to the codes where that takes few registers; of longer rows s is held,
-// which fp32 does, and y formed twice: fewer registers are more rows on a CU (2000 x 12288 bf16, rms with a sum 47.3 -> 45.0 us).
+// Rows of up to 8 LANES HOLD channels, LANES to a row.  y is held from the statistic to the codes where that takes few
+// registers; of longer rows s is held, which fp32 does, and y formed twice: fewer registers are more rows on a CU (2000
+// x 12288 bf16, rms with a sum 47.3 -> 45.0 us).
 template <typename T, int KIND, int LANES, int HOLD>
 __global__ void __launch_bounds__(256) norm_q8_kernel(NormQ8Dev<T> p) {
   constexpr int ROWS = 256 / LANES;
