@@ -126,3 +126,26 @@ def test_logprobs_of_differences_beyond_fp32(dtype, vocab, scale):
     x[5, 3] = -most
     tokens = torch.tensor([0, 0, 0, 0, 4, 3], dtype=torch.int32)
     _run(x, tokens, scale, 5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5, 1000, 12000, 40000, 126464])
+@pytest.mark.parametrize("scale", [65536.0, 1e8, 1e30])
+def test_logprobs_special_rows_of_large_scales(dtype, vocab, scale):
+    """Nothing left, a token outside the vocabulary, zeros of both signs, the type's ends; NaN and infinity reach their row alone."""
+    lowest = float(torch.finfo(TYPES[dtype]).min)
+    x = torch.randn(9, vocab, generator=_gen(7)).to(TYPES[dtype])
+    x[0] = -math.inf
+    x[2], x[2, 3] = 0.0, -0.0
+    x[2, 4] = -1.0
+    x[3] = lowest
+    x[4], x[4, 0] = lowest, -lowest
+    x[5], x[5, 2] = -math.inf, lowest
+    x[6], x[6, 1:3] = -math.inf, 1e-30
+    x[7, vocab - 1], x[8, 0] = math.inf, math.nan
+    tokens = torch.tensor([0, vocab, 3, 1, 0, 2, 1, 0, 1], dtype=torch.int32)
+    got = _outputs(9, 4)
+    B.dare_k_logprobs(x.cuda(), tokens.cuda(), *got, scale=float(np.float32(scale)))
+    _check(x[:7], tokens[:7], float(np.float32(scale)), 4, [t[:7] for t in got])
+    assert torch.isnan(got[0][7:]).all() and torch.isnan(got[1][7:]).all()
+    assert (got[2][7:] == -1).all() and torch.isnan(got[3][7:]).all()
